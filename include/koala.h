@@ -414,6 +414,112 @@ koala_status koala_train_medusa_head_step(void *hip_stream, int n_rows, int hidd
                                           const float *grad_d, float lr, void *workspace,
                                           size_t workspace_bytes);
 
+/* ---------------------------------------------------------------------------------------------
+ * Projections in 8-bit integers.  These calls need no koala_ctx and only enqueue kernels.  A Linear weight is
+ * int8 [out_features, in_features] with a scale per output channel, W[n][k] = w_scale[n] * w[n][k]; activations
+ * are int8 rows with a scale each, made by koala_quantize_rows.  Sums of products are exact (32-bit integers).
+ * Strides are in elements and may be larger than a row; rows begin on 16 bytes.
+ * --------------------------------------------------------------------------------------------- */
+enum { KOALA_ROWS_PLAIN = 0, KOALA_ROWS_NORM = 1, KOALA_ROWS_SWIGLU = 2 };
+
+/* Rows to 8 bits: v[r][c], c < cols, is
+ *   KOALA_ROWS_PLAIN   x[r][c]
+ *   KOALA_ROWS_NORM    x[r][c] * rsqrt(mean over the row of x^2 + eps) * gain[c]
+ *   KOALA_ROWS_SWIGLU  SiLU(x[r][2c]) * x[r][2c + 1] (gate and up interleaved, as wgu gives them)
+ * in fp32, scale[r] = (largest |v[r][c]|) / 127 (1 where that is zero), q[r][c] = v[r][c] / scale[r] rounded to the
+ * nearest whole number, ties to even.  A row with a value that is not finite gets the scale not-a-number (and with it
+ * every product of the row).
+ *   x      device [rows, cols] (SWIGLU: [rows, 2 cols]) of x_dtype, x_stride elements a row;
+ *   gain   device [cols] of gain_dtype (NORM; otherwise ignored);
+ *   q      device int8 [rows], q_stride a row, q_stride >= cols rounded up to 16: the bytes up to there are written zero;
+ *   scale  device fp32 [rows]. */
+koala_status koala_quantize_rows(void *hip_stream, int form, int x_dtype, int rows, int cols, const void *x,
+                                 int64_t x_stride, const void *gain, int gain_dtype, float eps, int8_t *q,
+                                 int64_t q_stride, float *scale);
+
+/* Bytes of device workspace koala_linear_quantized needs for these sizes (16-byte aligned; may be 0). */
+koala_status koala_linear_workspace_bytes(int rows, int out_features, int in_features, size_t *out);
+
+/* y[r][n] = q_scale[r] * w_scale[n] * sum_k q[r][k] w[n][k] (+ add[r][n]), rounded once where y is bfloat16.
+ *   in_features a multiple of 16 and at most 131056 (the sum fits 32 bits for all int8 values); rows and out_features any;
+ *   add    device, the type and stride of y, may be NULL and may be y itself (a residual stream updated in place);
+ *   y      device [rows, out_features] of y_dtype. */
+koala_status koala_linear_quantized(void *hip_stream, int rows, int out_features, int in_features, const int8_t *q,
+                                    int64_t q_stride, const float *q_scale, const int8_t *w, int64_t w_stride,
+                                    const float *w_scale, int y_dtype, const void *add, void *y, int64_t y_stride,
+                                    void *workspace, size_t workspace_bytes);
+
+/* ---------------------------------------------------------------------------------------------
+ * Paged cache in 4 bits.  Keys (rotated) and values of all layers in pools of pages; a page holds page_size slots
+ * of every key head of one layer, and page_table says which page of the pools holds slots
+ * i * page_size .. (i + 1) * page_size - 1 of a sequence (the same page number in every layer).
+ *   k, v              device uint8 [n_layers][n_pages][n_kv_heads][page_size][head_dim / 2]: two codes a byte, the
+ *                     lower dimension in the lower half.  A code is a sign (8), two bits of exponent, one of mantissa:
+ *                     0, 1/2, 1, 3/2, 2, 3, 4, 6
+ *   k_scale, v_scale  device uint8 [n_layers][n_pages][n_kv_heads][page_size][head_dim / 32]: the power of two that 32
+ *                     neighbouring dimensions share, its exponent plus 127; 255: all 32 are not-a-number
+ *   page_table        device int32 [max_batch][pages_per_seq], entries 0 .. n_pages - 1 for every slot in use
+ *   ctx_len           device int32 [max_batch]: committed slots C_b; new rows go to slots C_b, C_b + 1, ...
+ * page_size 16, 32, 64, 128 or 256; head_dim 64 or 128.  The pools need not be cleared.  Calls on one cache are to be
+ * ordered like those on one context.  The struct is read during a call only.
+ * --------------------------------------------------------------------------------------------- */
+typedef struct {
+    void *k, *v, *k_scale, *v_scale;
+    int n_layers, n_pages, page_size, n_kv_heads, head_dim;
+    int max_batch, pages_per_seq;
+    const int32_t *page_table;
+    int32_t *ctx_len;
+} koala_paged_kv;
+
+/* Rotate and append: row i of sequence b (i < rows) goes to slot C_b + i of `layer`, its keys and queries rotated for
+ * position C_b + (depth ? depth[i] : i) (halves pairing, r7: x1 c - x2 s, x2 c + x1 s with c, s from the tables), its
+ * keys and values to 4 bits: a block's exponent is that of its largest magnitude's power of two less 2, one more where
+ * the magnitude is above 7/4 of that power, and at least -100; codes are the nearest, ties to the even one.  ctx_len stays as it is.
+ *   dtype    type of q, k, v and q_out (KOALA_BF16 or KOALA_FP32)
+ *   q, k, v  device [batch * rows][heads][head_dim], *_stride elements a row (they may be parts of one array);
+ *            n_heads = 0: no queries (q and q_out ignored)
+ *   n_new    device int32 [batch] or NULL: rows i >= n_new[b] of sequence b are padding
+ *   depth    device int32 [rows] or NULL (a tree's node depths)
+ *   rope_cos, rope_sin  device fp32 [rope_rows][head_dim / 2]
+ *   q_out    device [batch * rows][n_heads][head_dim], dense
+ * Nothing is written for padding, for positions outside the tables, and for slots that have no page. */
+koala_status koala_paged_append(const koala_paged_kv *kv, void *hip_stream, int layer, int batch, int rows, int dtype,
+                                int n_heads, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                const void *v, int64_t v_stride, const int32_t *n_new, const int32_t *depth,
+                                const float *rope_cos, const float *rope_sin, int rope_rows, void *q_out);
+
+/* Slots start[b] .. start[b] + n - 1 (start NULL: 0) of layers layer .. layer + n_layers - 1 as the values they stand
+ * for: k_out, v_out device [n_layers][batch][n][n_kv_heads][head_dim] of dtype, exact in either.  Slots without a page
+ * read as zero. */
+koala_status koala_paged_read(const koala_paged_kv *kv, void *hip_stream, int layer, int n_layers, int batch,
+                              const int32_t *start, int n, int dtype, void *k_out, void *v_out);
+
+/* Bytes of device workspace koala_paged_attend needs (any batch and rows). */
+koala_status koala_paged_workspace_bytes(const koala_paged_kv *kv, size_t *out);
+
+/* Attention of `rows` (1..KOALA_MAX_NODES) new rows a sequence over one layer of the cache, which already holds the
+ * new rows' own keys and values: out = softmax(scale * q k^T) v over the C_b committed slots and the new slots that the
+ * row's mask names.  Query head h reads key head h / (n_heads / n_kv_heads).
+ *   q     device [batch * rows][n_heads][head_dim] of dtype, rotated, q_stride elements a row
+ *   mask  device uint64, mask[b * mask_stride + i]: bit j set if row i sees new row j (mask_stride 0: one tree for all;
+ *         bits from `rows` on are ignored), or NULL: row i sees new rows 0 .. i.  A row that sees no slot at all gives zeros
+ *   max_len  slots at or past it are not read (0: as many as the table has).  A caller that knows its longest
+ *         sequence, C_b + rows, need not pass it: the lengths are taken from ctx_len
+ *   out   device [batch * rows][n_heads][head_dim] of dtype, dense
+ * The cache's values and bfloat16 queries are exact in the products; probabilities carry 11 significant bits, and 24 where out
+ * is fp32, as fp32 queries do; sums are fp32.  The workspace
+ * (16-byte aligned) need not be cleared and holds nothing between calls. */
+koala_status koala_paged_attend(const koala_paged_kv *kv, void *hip_stream, int layer, int batch, int rows, int dtype,
+                                int n_heads, const void *q, int64_t q_stride, const uint64_t *mask, int64_t mask_stride,
+                                float scale, int max_len, void *out, void *workspace, size_t workspace_bytes);
+
+/* Commit an accepted path (koala_accept_prefix with commit 0, koala_accept_sample) in every layer: the rows of its nodes move to
+ * slots C_b .. C_b + a, and new_len[b] = C_b + a + 1.
+ *   accept_len device int32 [batch], accept_path device int32 [batch][path_stride]: node ids, growing, from the root
+ *   new_len    device int32 [batch] (out); may be ctx_len itself */
+koala_status koala_paged_commit(const koala_paged_kv *kv, void *hip_stream, int batch, const int32_t *accept_len,
+                                const int32_t *accept_path, int path_stride, int32_t *new_len);
+
 /* Text of the last error on this context ("" if none); valid until the next call. */
 const char *koala_last_error(const koala_ctx *ctx);
 

@@ -13,7 +13,12 @@ EXPORTS = ("koala_create", "koala_workspace_bytes", "koala_bind", "koala_draft_e
            "koala_measure_stream_read", "koala_profile_begin",
            "koala_profile_end", "koala_train_workspace_bytes", "koala_train_disc_step", "koala_train_gen_grad",
            "koala_train_medusa_workspace_bytes", "koala_train_medusa_head_forward", "koala_train_medusa_head_step",
+           "koala_quantize_rows", "koala_linear_workspace_bytes", "koala_linear_quantized", "koala_paged_append",
+           "koala_paged_read", "koala_paged_workspace_bytes", "koala_paged_attend", "koala_paged_commit",
            "koala_last_error", "koala_destroy")
+
+KOALA_ROWS_PLAIN, KOALA_ROWS_NORM, KOALA_ROWS_SWIGLU = 0, 1, 2
+_ROW_FORMS = {"plain": KOALA_ROWS_PLAIN, "norm": KOALA_ROWS_NORM, "swiglu": KOALA_ROWS_SWIGLU}
 
 _STATUS = {0: "KOALA_OK", -1: "KOALA_E_NULL", -2: "KOALA_E_SHAPE", -3: "KOALA_E_ALIGN",
            -4: "KOALA_E_CAPACITY", -5: "KOALA_E_UNSUPPORTED", -6: "KOALA_E_WORKSPACE",
@@ -67,6 +72,13 @@ class _KV(C.Structure):
                 ("draft_v", C.c_void_p), ("capacity", C.c_int), ("ctx_len", C.c_void_p)]
 
 
+class _PagedKV(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n_layers", C.c_int), ("n_pages", C.c_int), ("page_size", C.c_int), ("n_kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("max_batch", C.c_int), ("pages_per_seq", C.c_int), ("page_table", C.c_void_p),
+                ("ctx_len", C.c_void_p)]
+
+
 def library_path() -> str:
     return os.path.join(os.path.dirname(os.path.abspath(__file__)), "libkoala.so")
 
@@ -112,11 +124,20 @@ def load_library():
     lib.koala_train_medusa_workspace_bytes.argtypes = [ip, ip, ip, C.POINTER(C.c_size_t)]
     lib.koala_train_medusa_head_forward.argtypes = [vp, ip, ip, ip, ip, C.POINTER(vp), vp, vp, vp, C.c_size_t, vp]
     lib.koala_train_medusa_head_step.argtypes = [vp, ip, ip, ip, ip, C.POINTER(vp), vp, vp, vp, fl, vp, C.c_size_t]
+    i64, paged = C.c_int64, C.POINTER(_PagedKV)
+    lib.koala_quantize_rows.argtypes = [vp, ip, ip, ip, ip, vp, i64, vp, ip, fl, vp, i64, vp]
+    lib.koala_linear_workspace_bytes.argtypes = [ip, ip, ip, C.POINTER(C.c_size_t)]
+    lib.koala_linear_quantized.argtypes = [vp, ip, ip, ip, vp, i64, vp, vp, i64, vp, ip, vp, vp, i64, vp, C.c_size_t]
+    lib.koala_paged_append.argtypes = [paged, vp, ip, ip, ip, ip, ip, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, ip, vp]
+    lib.koala_paged_read.argtypes = [paged, vp, ip, ip, ip, vp, ip, ip, vp, vp]
+    lib.koala_paged_workspace_bytes.argtypes = [paged, C.POINTER(C.c_size_t)]
+    lib.koala_paged_attend.argtypes = [paged, vp, ip, ip, ip, ip, ip, vp, i64, vp, i64, fl, ip, vp, vp, C.c_size_t]
+    lib.koala_paged_commit.argtypes = [paged, vp, ip, vp, vp, ip, vp]
     lib.koala_last_error.argtypes = [vp]
     lib.koala_last_error.restype = C.c_char_p
     lib.koala_destroy.argtypes = [vp]
     lib.koala_destroy.restype = None
-    for n in EXPORTS[:20]:
+    for n in EXPORTS[:-2]:
         getattr(lib, n).restype = C.c_int
     _LIB = lib
     return lib
@@ -369,3 +390,252 @@ class MedusaHeadTrainer:
                                                    _ptr(grad_d), float(lr), _ptr(ws), ws.numel())
         if rc != 0:
             raise KoalaError(rc, "koala_train_medusa_head_step")
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# 8-bit projections and the 4-bit paged cache.  A tensor's type, place and layout are known here only, so they are
+# checked here; sizes, strides and alignment are checked by the library.
+# ---------------------------------------------------------------------------------------------------------------
+def _refuse(name, msg):
+    raise KoalaError(STATUS_BY_NAME[name], msg)
+
+
+def _dtype(t, what):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return KOALA_BF16
+    if t.dtype != torch.float32:
+        _refuse("KOALA_E_UNSUPPORTED", f"{what}: bfloat16 or float32 wanted, got {t.dtype}")
+    return KOALA_FP32
+
+
+def _of(t, dtype, what, shape=None):
+    """The address of a dense device tensor of the given type and shape."""
+    if t.dtype != dtype or not t.is_cuda:
+        _refuse("KOALA_E_UNSUPPORTED", f"{what}: {dtype} on the device wanted, got {t.dtype} on {t.device}")
+    if not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+        _refuse("KOALA_E_SHAPE", f"{what}: dense {shape if shape is not None else ''} wanted, got {tuple(t.shape)} strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _matrix(t, what):
+    """Address and row stride of a device matrix whose rows are dense."""
+    if not t.is_cuda:
+        _refuse("KOALA_E_UNSUPPORTED", f"{what}: a device tensor wanted")
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        _refuse("KOALA_E_SHAPE", f"{what}: a matrix of dense rows wanted, got {tuple(t.shape)} strides {t.stride()}")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+
+
+def _heads(t, batch, rows, head_dim, what):
+    """Number of heads and row stride of a device tensor [batch, rows, heads, head_dim] whose rows are dense and evenly spaced."""
+    if not t.is_cuda:
+        _refuse("KOALA_E_UNSUPPORTED", f"{what}: a device tensor wanted")
+    sb, sr, sh, sd = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
+    if t.dim() != 4 or t.shape[0] != batch or t.shape[1] != rows or t.shape[3] != head_dim or sd != 1 or (t.shape[2] > 1 and sh != head_dim):
+        _refuse("KOALA_E_SHAPE", f"{what}: [{batch}, {rows}, heads, {head_dim}] of dense rows wanted, got {tuple(t.shape)} strides {t.stride()}")
+    if rows > 1:
+        if batch > 1 and sb != rows * sr:
+            _refuse("KOALA_E_SHAPE", f"{what}: rows are not evenly spaced (strides {t.stride()})")
+        return t.shape[2], sr
+    return t.shape[2], (sb if batch > 1 else t.shape[2] * head_dim)
+
+
+def _raw_stream(stream):
+    import torch
+    return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+
+
+class _Workspaces:
+    """One device buffer a stream, so that calls on different streams do not share one; allocated on the stream it is used on."""
+
+    def __init__(self):
+        self._by_stream = {}
+
+    def get(self, raw, need, device, stream):
+        ws = self._by_stream.get(raw)
+        if ws is None or ws.numel() < need:
+            import torch
+            with torch.cuda.stream(stream):
+                ws = self._by_stream[raw] = torch.empty(need, dtype=torch.uint8, device=device)
+        return ws
+
+
+def quantize_rows(x, q, scale, form="plain", gain=None, eps=1e-6, stream=None):
+    """Rows of x (bfloat16 or float32) to int8 rows q with a scale each (koala_quantize_rows).  form "norm": RMSNorm with `gain` first;
+    "swiglu": SiLU(gate) * up of x's interleaved pairs.  q may be wider than the row: bytes up to the next 16 are zeroed."""
+    import torch
+    if form not in _ROW_FORMS:
+        _refuse("KOALA_E_UNSUPPORTED", f"form {form!r}")
+    xt = _dtype(x, "x")
+    xp, xs = _matrix(x, "x")
+    qp, qs = _matrix(q, "q")
+    rows, cols = x.shape
+    if form == "swiglu":
+        if cols % 2:
+            _refuse("KOALA_E_SHAPE", "x: pairs of gate and up wanted")
+        cols //= 2
+    if q.dtype != torch.int8:
+        _refuse("KOALA_E_UNSUPPORTED", f"q: int8 wanted, got {q.dtype}")
+    if q.shape[0] != rows or q.shape[1] < cols:
+        _refuse("KOALA_E_SHAPE", f"q: [{rows}, {cols}] wanted, got {tuple(q.shape)}")
+    gp, gt = 0, 0
+    if form == "norm" and gain is not None:
+        gt = _dtype(gain, "gain")
+        gp = _of(gain, gain.dtype, "gain", (cols,))
+    rc = load_library().koala_quantize_rows(_raw_stream(stream), _ROW_FORMS[form], xt, rows, cols, xp, xs, gp, gt, eps, qp, qs,
+                                            _of(scale, torch.float32, "scale", (rows,)))
+    if rc != 0:
+        raise KoalaError(rc, "koala_quantize_rows")
+
+
+class QuantizedLinear:
+    """A Linear weight in 8 bits: w int8 [out_features, in_features] (rows may be strided) and w_scale fp32 [out_features], borrowed."""
+
+    def __init__(self, w, w_scale):
+        import torch
+        self.lib = load_library()
+        if w.dtype != torch.int8:
+            _refuse("KOALA_E_UNSUPPORTED", f"w: int8 wanted, got {w.dtype}")
+        self.w, self.w_scale = w, w_scale
+        self.out_features, self.in_features = w.shape
+        self._wp, self._ws = _matrix(w, "w")
+        self._sp = _of(w_scale, torch.float32, "w_scale", (self.out_features,))
+        self._need, self._workspaces = {}, _Workspaces()
+
+    def _workspace_bytes(self, rows):
+        need = C.c_size_t()
+        rc = self.lib.koala_linear_workspace_bytes(rows, self.out_features, self.in_features, C.byref(need))
+        if rc != 0:
+            raise KoalaError(rc, f"koala_linear_workspace_bytes: {rows} rows, weight {tuple(self.w.shape)}")
+        self._need[rows] = need.value
+        return need.value
+
+    def forward(self, q, scale, y, add=None, stream=None):
+        """y = scale * w_scale * (q w^T) (+ add, which may be y): q int8 [rows, >= in_features] and scale from quantize_rows, y
+        bfloat16 or float32 [rows, out_features]."""
+        import torch
+        rows = q.shape[0]
+        if q.dtype != torch.int8:
+            _refuse("KOALA_E_UNSUPPORTED", f"q: int8 wanted, got {q.dtype}")
+        qp, qs = _matrix(q, "q")
+        yt = _dtype(y, "y")
+        yp, ys = _matrix(y, "y")
+        if q.shape[1] < self.in_features or tuple(y.shape) != (rows, self.out_features):
+            _refuse("KOALA_E_SHAPE", f"q {tuple(q.shape)}, y {tuple(y.shape)} for a weight {tuple(self.w.shape)}")
+        ap = 0
+        if add is not None:
+            ap, a_stride = _matrix(add, "add")
+            if add.dtype != y.dtype or add.shape != y.shape or (rows > 1 and a_stride != ys):
+                _refuse("KOALA_E_SHAPE", "add: the type, shape and strides of y wanted")
+        need = self._need.get(rows)
+        if need is None:
+            need = self._workspace_bytes(rows)
+        wp = 0
+        raw = _raw_stream(stream)
+        if need:
+            wp = self._workspaces.get(raw, need, y.device, stream).data_ptr()
+        rc = self.lib.koala_linear_quantized(raw, rows, self.out_features, self.in_features, qp, qs,
+                                             _of(scale, torch.float32, "scale", (rows,)), self._wp, self._ws, self._sp, yt, ap, yp, ys,
+                                             wp, need)
+        if rc != 0:
+            raise KoalaError(rc, "koala_linear_quantized")
+
+
+class PagedCache:
+    """A paged key/value cache in 4 bits over the caller's device memory (koala_paged_kv): k, v uint8 [layers, pages, kv_heads,
+    page_size, head_dim / 2], k_scale, v_scale uint8 [..., head_dim / 32], page_table int32 [max_batch, pages_per_seq], ctx_len
+    int32 [max_batch].  `alloc_paged_cache` makes the pools."""
+
+    def __init__(self, k, v, k_scale, v_scale, page_table, ctx_len):
+        import torch
+        self.lib = load_library()
+        if k.dim() != 5 or page_table.dim() != 2:
+            _refuse("KOALA_E_SHAPE", "k: five dimensions wanted; page_table: two")
+        layers, pages, heads, page, half = k.shape
+        scales = (layers, pages, heads, page, half // 16)
+        u8, i32 = torch.uint8, torch.int32
+        self.n_layers, self.n_kv_heads, self.head_dim = layers, heads, 2 * half
+        self.max_batch = page_table.shape[0]
+        self._kv = _PagedKV(_of(k, u8, "k"), _of(v, u8, "v", tuple(k.shape)), _of(k_scale, u8, "k_scale", scales),
+                            _of(v_scale, u8, "v_scale", scales), layers, pages, page, heads, 2 * half, self.max_batch,
+                            page_table.shape[1], _of(page_table, i32, "page_table"), _of(ctx_len, i32, "ctx_len", (self.max_batch,)))
+        self._ref = C.byref(self._kv)
+        self._keep = (k, v, k_scale, v_scale, page_table, ctx_len)   # the library reads them in every call
+        need = C.c_size_t()
+        self._check(self.lib.koala_paged_workspace_bytes(self._ref, C.byref(need)), "koala_paged_workspace_bytes")
+        self._need, self._workspaces = need.value, _Workspaces()
+
+    @staticmethod
+    def _check(rc, name):
+        if rc != 0:
+            raise KoalaError(rc, name)
+
+    def append(self, layer, q, k, v, q_out, rope_cos, rope_sin, depth=None, n_new=None, stream=None):
+        """Rotate and append the new rows of every sequence: q [batch, rows, heads, head_dim] (may be None), k, v [batch, rows,
+        kv_heads, head_dim], possibly parts of one array; q_out dense.  See koala_paged_append."""
+        import torch
+        batch, rows = k.shape[0], k.shape[1]
+        dt = _dtype(k, "k")
+        hk, ldk = _heads(k, batch, rows, self.head_dim, "k")
+        hv, ldv = _heads(v, batch, rows, self.head_dim, "v")
+        if hk != self.n_kv_heads or hv != hk or v.dtype != k.dtype:
+            _refuse("KOALA_E_SHAPE", f"k, v: {self.n_kv_heads} heads of one type wanted")
+        heads, ldq, qp, op = 0, 0, 0, 0
+        if q is not None:
+            heads, ldq = _heads(q, batch, rows, self.head_dim, "q")
+            if q.dtype != k.dtype:
+                _refuse("KOALA_E_UNSUPPORTED", "q: the type of k wanted")
+            qp, op = q.data_ptr(), _of(q_out, k.dtype, "q_out", (batch, rows, heads, self.head_dim))
+        half = self.head_dim // 2
+        table = (rope_cos.shape[0], half)
+        self._check(self.lib.koala_paged_append(
+            self._ref, _raw_stream(stream), layer, batch, rows, dt, heads, qp, ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+            0 if n_new is None else _of(n_new, torch.int32, "n_new", (batch,)),
+            0 if depth is None else _of(depth, torch.int32, "depth", (rows,)), _of(rope_cos, torch.float32, "rope_cos", table),
+            _of(rope_sin, torch.float32, "rope_sin", table), table[0], op), "koala_paged_append")
+
+    def read(self, layer, start, k_out, v_out, stream=None):
+        """Slots start[b] .. (start None: from 0) of one layer (k_out, v_out [batch, n, kv_heads, head_dim]) or of all
+        (layer None: [layers, batch, n, kv_heads, head_dim]) as the values they stand for, bfloat16 or float32."""
+        import torch
+        dt = _dtype(k_out, "k_out")
+        shape = tuple(k_out.shape)
+        if len(shape) != (5 if layer is None else 4) or shape[-2:] != (self.n_kv_heads, self.head_dim) or (layer is None and shape[0] != self.n_layers):
+            _refuse("KOALA_E_SHAPE", f"k_out: got {shape}")
+        batch, n = shape[-4], shape[-3]
+        self._check(self.lib.koala_paged_read(
+            self._ref, _raw_stream(stream), layer or 0, self.n_layers if layer is None else 1, batch,
+            0 if start is None else _of(start, torch.int32, "start", (batch,)), n, dt, _of(k_out, k_out.dtype, "k_out"),
+            _of(v_out, k_out.dtype, "v_out", shape)), "koala_paged_read")
+
+    def attend(self, layer, q, out, mask=None, scale=None, max_len=0, stream=None):
+        """Attention of the new rows (already appended) over the cache: q [batch, rows <= 64, heads, head_dim] rotated, out dense.
+        mask: int64 [rows] or [batch, rows], bit j of a row's set if it sees new row j (tree_masks); None: rows up to its own."""
+        import torch
+        if q.dim() != 4:
+            _refuse("KOALA_E_SHAPE", f"q: [batch, rows, heads, head_dim] wanted, got {tuple(q.shape)}")
+        batch, rows = q.shape[0], q.shape[1]
+        dt = _dtype(q, "q")
+        heads, ldq = _heads(q, batch, rows, self.head_dim, "q")
+        mp, ms = 0, 0
+        if mask is not None:
+            per_seq = mask.dim() == 2
+            mp, ms = _of(mask, torch.int64, "mask", (batch, rows) if per_seq else (rows,)), (rows if per_seq else 0)
+        raw = _raw_stream(stream)
+        ws = self._workspaces.get(raw, self._need, q.device, stream)
+        self._check(self.lib.koala_paged_attend(
+            self._ref, raw, layer, batch, rows, dt, heads, q.data_ptr(), ldq, mp, ms,
+            self.head_dim ** -0.5 if scale is None else scale, max_len,
+            _of(out, q.dtype, "out", (batch, rows, heads, self.head_dim)), ws.data_ptr(), self._need), "koala_paged_attend")
+
+    def commit(self, accept_len, accept_path, new_len=None, stream=None):
+        """Move the accepted paths' rows behind the context in every layer; new_len (default: ctx_len itself) becomes the new lengths."""
+        import torch
+        batch = accept_len.shape[0]
+        if accept_path.dim() != 2:
+            _refuse("KOALA_E_SHAPE", "accept_path: [batch, depth + 1] wanted")
+        self._check(self.lib.koala_paged_commit(
+            self._ref, _raw_stream(stream), batch, _of(accept_len, torch.int32, "accept_len", (batch,)),
+            _of(accept_path, torch.int32, "accept_path", (batch, accept_path.shape[1])), accept_path.shape[1],
+            self._kv.ctx_len if new_len is None else _of(new_len, torch.int32, "new_len", (batch,))), "koala_paged_commit")

@@ -1,0 +1,914 @@
+// A paged key/value cache held in 4 bits: rows rotated and appended, read back, tree-masked attention over it, and the
+// accepted rows' commit (koala.h, "Paged cache in 4 bits").
+//
+// Format.  A row (one slot of one key head) is head_dim values in blocks of 32 that share a power of two; a value is one of
+// 0, 1/2, 1, 3/2, 2, 3, 4, 6 with a sign, times that power.  The chip converts to and from this format in one instruction for
+// two values, scale included, so a key costs half an instruction a value on its way into the matrix pipe; the values are exact
+// in bfloat16.  The block's exponent is that of its largest value less 2, and one more where the largest is above 7/4 of its
+// power of two: it then lies nearer to 4 of the doubled grid (8) than to 6 of this one.  (Normal values, root mean square error
+// over the values': 0.1118; always cutting off at 6, 0.1149; never, 0.1154.)
+#include "koala_internal.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+
+enum { BLOCK = 32, MIN_EXP = 27, NAN_EXP = 255 };   // exponents are stored plus 127; the smallest is 2^-100: no value is subnormal
+
+__device__ __forceinline__ float exp_scale(unsigned e) { return __uint_as_float(e << 23); }
+
+// where a slot of a sequence lies: its row number among a layer's rows of head 0, or -1 if it has none
+struct Pool {
+    uint8_t *k, *v, *ks, *vs;
+    const int32_t *table;
+    int n_pages, log_page, n_kv, pages_per_seq;
+    size_t layer_rows;   // n_pages * n_kv * page
+};
+__device__ __forceinline__ long slot_row(const Pool &p, int b, int slot) {
+    if (slot < 0 || (slot >> p.log_page) >= p.pages_per_seq) return -1;
+    const int page = p.table[(size_t)b * p.pages_per_seq + (slot >> p.log_page)];
+    if ((unsigned)page >= (unsigned)p.n_pages) return -1;
+    return (((long)page * p.n_kv) << p.log_page) + (slot & ((1 << p.log_page) - 1));
+}
+
+template <bool F32> __device__ __forceinline__ void load8(const void *src, size_t i, float *x) {
+    if (F32) {
+        const f32x4 a = ((const f32x4 *)((const float *)src + i))[0], b = ((const f32x4 *)((const float *)src + i))[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
+    } else {
+        const u32x4 a = *(const u32x4 *)((const bf16_t *)src + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(a[e] << 16); x[2 * e + 1] = __uint_as_float(a[e] & 0xFFFF0000u); }
+    }
+}
+__device__ __forceinline__ uint32_t bf_pair(float a, float b) {   // round to nearest even
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
+}
+template <bool F32> __device__ __forceinline__ void store8(void *dst, size_t i, const float *x) {
+    if (F32) {
+        ((f32x4 *)((float *)dst + i))[0] = (f32x4){x[0], x[1], x[2], x[3]};
+        ((f32x4 *)((float *)dst + i))[1] = (f32x4){x[4], x[5], x[6], x[7]};
+    } else {
+        *(u32x4 *)((bf16_t *)dst + i) = (u32x4){bf_pair(x[0], x[1]), bf_pair(x[2], x[3]), bf_pair(x[4], x[5]), bf_pair(x[6], x[7])};
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Append.  A lane holds eight dimensions of a head's first half and their rotary partners in the second, so a rotation needs no
+// exchange and a block of 32 is four neighbouring lanes.  A row's queries, keys and values are its n_heads + 2 n_kv heads in turn.
+// The rotation is computed product by product, without fused multiply-adds: a code then does not depend on how a compiler
+// contracts a sum.
+// ---------------------------------------------------------------------------------------------
+struct AppendArgs {
+    Pool p;
+    const int32_t *ctx_len, *n_new, *depth;
+    const float *cos, *sin;
+    int rope_rows, rows, rows_per_seq, n_heads;
+    const void *q, *k, *v;
+    size_t ldq, ldk, ldv;
+    void *q_out;
+};
+
+__device__ __forceinline__ unsigned quad_max(unsigned x) {   // over four neighbouring lanes
+    x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
+    return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));  // lanes 2 3 0 1
+}
+// eight values of a lane, its block's exponent agreed among four lanes, as codes; a block with a value that is not finite is
+// stored as not-a-number throughout
+__device__ __forceinline__ uint32_t encode8(const float *x, unsigned &e) {
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    top = quad_max(top);
+    if (top >= 0x7F800000u) {
+        e = NAN_EXP;
+        return 0u;
+    }
+    e = (unsigned)max((int)(top >> 23) + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0) - 2, (int)MIN_EXP);
+    const float s = exp_scale(e);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
+    return c;
+}
+
+template <int DH, bool F32> __global__ __launch_bounds__(256) void k_paged_append(AppendArgs a) {
+#pragma clang fp contract(off)
+    constexpr int LPH = DH / 16;   // lanes of a head
+    const unsigned per_row = (unsigned)(a.n_heads + 2 * a.p.n_kv) * LPH;
+    const unsigned at = blockIdx.x * 256 + threadIdx.x, row_ = at / per_row;
+    if (row_ >= (unsigned)a.rows) return;
+    const int row = (int)row_, u = (int)(at - row_ * per_row), hs = u / LPH, j = u % LPH;
+    const int b = row / a.rows_per_seq, i = row - b * a.rows_per_seq;
+    const bool is_q = hs < a.n_heads, is_k = !is_q && hs < a.n_heads + a.p.n_kv;
+    const int h = is_q ? hs : is_k ? hs - a.n_heads : hs - a.n_heads - a.p.n_kv;
+    const void *src = is_q ? a.q : is_k ? a.k : a.v;
+    const size_t from = (size_t)row * (is_q ? a.ldq : is_k ? a.ldk : a.ldv) + (size_t)h * DH + 8 * j;
+    float x[2][8];
+    load8<F32>(src, from, x[0]);
+    load8<F32>(src, from + DH / 2, x[1]);
+    const int ctx = a.ctx_len[b], slot = ctx + i, pos = ctx + (a.depth ? a.depth[i] : i);
+    // (slots of a negative length are outside the table)
+    if ((a.n_new && i >= a.n_new[b]) || ctx < 0 || pos < 0 || pos >= a.rope_rows) return;
+    if (is_q || is_k) {
+        float c[8], s[8];
+        load8<true>(a.cos, (size_t)pos * (DH / 2) + 8 * j, c);
+        load8<true>(a.sin, (size_t)pos * (DH / 2) + 8 * j, s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float p = x[0][e] * c[e], q = x[1][e] * s[e], r = x[1][e] * c[e], t = x[0][e] * s[e];
+            x[0][e] = p - q;
+            x[1][e] = r + t;
+        }
+    }
+    const long r0 = slot_row(a.p, b, slot);
+    if (r0 < 0) return;   // the same for all lanes of a row
+    if (is_q) {
+        const size_t to = ((size_t)row * a.n_heads + h) * DH + 8 * j;
+        store8<F32>(a.q_out, to, x[0]);
+        store8<F32>(a.q_out, to + DH / 2, x[1]);
+        return;
+    }
+    const size_t r = (size_t)r0 + ((size_t)h << a.p.log_page);
+    uint8_t *codes = (is_k ? a.p.k : a.p.v) + r * (DH / 2) + 4 * j;
+    uint8_t *scales = (is_k ? a.p.ks : a.p.vs) + r * (DH / BLOCK) + j / 4;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        unsigned e;
+        const uint32_t c = encode8(x[half], e);
+        *(uint32_t *)(codes + half * (DH / 4)) = c;
+        if (j % 4 == 0) scales[half * (DH / 64)] = (uint8_t)e;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Read back: eight values a lane
+// ---------------------------------------------------------------------------------------------
+struct ReadArgs {
+    Pool p;
+    const int32_t *start;
+    unsigned batch, n, layers;
+    void *k_out, *v_out;
+};
+__device__ __forceinline__ f32x2 decode2(uint32_t c, float s, int sel) {
+    switch (sel) {
+    case 0: return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0);
+    case 1: return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
+    case 2: return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2);
+    default: return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
+    }
+}
+template <int DH, bool F32> __global__ __launch_bounds__(256) void k_paged_read(ReadArgs a) {
+    constexpr int LPH = DH / 8;
+    const unsigned at = blockIdx.x * 256 + threadIdx.x, per_row = (unsigned)a.p.n_kv * LPH;
+    const unsigned row = at / per_row, seq = row / a.n, layer = seq / a.batch;   // row: (layer, sequence, slot)
+    if (layer >= (unsigned)a.layers) return;
+    const int u = (int)(at - row * per_row), h = u / LPH, j = u % LPH;
+    const int i = (int)(row - seq * a.n), b = (int)(seq - layer * a.batch);
+    const long slot = (long)(a.start ? a.start[b] : 0) + i;
+    const long r0 = slot > 0x7FFFFFFFl ? -1 : slot_row(a.p, b, (int)slot);
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+        float x[8];
+        if (r0 >= 0) {
+            const size_t r = layer * a.p.layer_rows + (size_t)r0 + ((size_t)h << a.p.log_page);
+            const uint32_t c = *(const uint32_t *)((kv ? a.p.v : a.p.k) + r * (DH / 2) + 4 * j);
+            const unsigned e = (kv ? a.p.vs : a.p.ks)[r * (DH / BLOCK) + j / 4];
+            const float s = exp_scale(e);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                const f32x2 d = decode2(c, s, z);
+                x[2 * z] = e == NAN_EXP ? __builtin_nanf("") : d[0];
+                x[2 * z + 1] = e == NAN_EXP ? __builtin_nanf("") : d[1];
+            }
+        } else {
+#pragma unroll
+            for (int z = 0; z < 8; ++z) x[z] = 0.f;
+        }
+        store8<F32>(kv ? a.v_out : a.k_out, ((size_t)row * a.p.n_kv + h) * DH + 8 * j, x);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Commit.  A lane moves one 16-byte piece (or the exponents) of every accepted row of a key head, in path order: node ids grow
+// along a path, so the slot a row moves to (its place on the path) is never one that a later row still has to be read from.
+// ---------------------------------------------------------------------------------------------
+struct CommitArgs {
+    Pool p;
+    const int32_t *ctx_len, *accept_len, *accept_path;
+    int32_t *new_len;   // null: written by a launch of its own (new_len is ctx_len itself)
+    int path_stride;
+    unsigned batch, layers;
+};
+template <int DH> __global__ __launch_bounds__(256) void k_paged_commit(CommitArgs a) {
+    constexpr int PIECES = DH / 32;            // of 16 bytes, keys or values
+    constexpr int LPH = 2 * PIECES + 2;
+    const unsigned at = blockIdx.x * 256 + threadIdx.x, head = at / LPH, seq = head / a.p.n_kv, layer = seq / a.batch;
+    if (layer >= (unsigned)a.layers) return;   // head: (layer, sequence, key head)
+    const int j = (int)(at - head * LPH), h = (int)(head - seq * a.p.n_kv), b = (int)(seq - layer * a.batch);
+    const int ctx = a.ctx_len[b], n = min(a.accept_len[b], a.path_stride - 1);
+    if (a.new_len && layer == 0 && h == 0 && j == 0) a.new_len[b] = ctx + a.accept_len[b] + 1;
+    const size_t base = layer * a.p.layer_rows + ((size_t)h << a.p.log_page);
+    constexpr int AHEAD = 8;
+    for (int i0 = 1; i0 <= n; i0 += AHEAD) {
+        u32x4 x[AHEAD];
+        uint32_t e[AHEAD];
+        long to[AHEAD];
+#pragma unroll
+        for (int z = 0; z < AHEAD; ++z) {
+            const int i = i0 + z;
+            to[z] = -1;
+            if (i > n) continue;
+            const int node = a.accept_path[(size_t)b * a.path_stride + i];
+            if (node <= i || ctx < 0) continue;   // in its place already (or none)
+            const long s = slot_row(a.p, b, ctx + node), d = slot_row(a.p, b, ctx + i);
+            if (s < 0 || d < 0) continue;
+            to[z] = (long)base + d;
+            const size_t from = base + (size_t)s;
+            if (j < 2 * PIECES) x[z] = ((const u32x4 *)((j < PIECES ? a.p.k : a.p.v) + from * (DH / 2)))[j % PIECES];
+            else if (DH == 128) e[z] = *(const uint32_t *)((j == 2 * PIECES ? a.p.ks : a.p.vs) + from * 4);
+            else e[z] = *(const uint16_t *)((j == 2 * PIECES ? a.p.ks : a.p.vs) + from * 2);
+        }
+#pragma unroll
+        for (int z = 0; z < AHEAD; ++z) {
+            if (to[z] < 0) continue;
+            if (j < 2 * PIECES) ((u32x4 *)((j < PIECES ? a.p.k : a.p.v) + to[z] * (DH / 2)))[j % PIECES] = x[z];
+            else if (DH == 128) *(uint32_t *)((j == 2 * PIECES ? a.p.ks : a.p.vs) + to[z] * 4) = e[z];
+            else *(uint16_t *)((j == 2 * PIECES ? a.p.ks : a.p.vs) + to[z] * 2) = (uint16_t)e[z];
+        }
+    }
+}
+__global__ void k_paged_advance(int32_t *len, const int32_t *accept_len, int batch) {
+    const int b = blockIdx.x * 256 + threadIdx.x;
+    if (b < batch) len[b] += accept_len[b] + 1;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Attention.  O = softmax(scale Q K^T, masked) V for up to 64 rows a sequence, with one pass over the keys and the running
+// maximum and sum of a softmax.  The rows of all query heads that share a key head are one set of rows (row t, head g: t * G + g)
+// in tiles of 16; an item is (sequence, key head, MT row tiles).
+//
+// The work is the items' steps of 32 keys laid end to end, and workgroup w of `wgs` takes [w * total / wgs, (w + 1) * total / wgs):
+// every compute unit gets the same number of keys whatever the sequences' lengths, which only the device knows.  An item that one
+// workgroup has taken whole is finished there; of the others each workgroup leaves a partial result (at most two a workgroup),
+// and a second launch joins them.  Within a workgroup four waves take the steps in turn and meet in LDS at the item's end.
+//
+// A step of a wave: S^T[key][row] = K Q^T on the matrix pipe (a lane's 16 bytes of codes are 32 dimensions of a key: the
+// contraction's order over the head dimension is chosen so that they are four operands as they lie), softmax in powers of two,
+// O^T += V^T P^T with V converted to 16 bits, put into LDS as rows and read back through the transposing load.  For bfloat16
+// outputs P and V are fp16: V is exact as long as its exponents are (which a wave asks of every step), P has 11 bits, an eighth of
+// the output's own rounding.  For fp32 outputs, and for the steps whose values leave fp16's range, V is bfloat16, exact always, and P the
+// sum of three bfloat16 pieces; so are fp32 queries.  bfloat16 queries are exact.
+// ---------------------------------------------------------------------------------------------
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+typedef u32x4 __attribute__((may_alias)) u32x4_alias;
+typedef f32x4 __attribute__((may_alias)) f32x4_alias;
+typedef float __attribute__((may_alias)) f32_alias;
+
+constexpr int WAVES = 4, NT = 64 * WAVES, STEP = 32;
+constexpr int MAX_PARTS = 32;   // workgroups an item is spread over, on average at most
+constexpr float LOG2E = 1.44269504088896340736f;
+// block exponents (plus 127) whose values fp16 holds exactly: 1/2 2^-23 is its smallest, 6 2^13 below its largest
+constexpr unsigned HALF_LO = 127 - 23, HALF_HI = 127 + 13;
+
+__device__ __forceinline__ float lane_groups_max(float x) {
+    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float lane_groups_sum(float x) {
+    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(q[0]) + __uint_as_float(q[1]);
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// eight values as the sum of N bfloat16 pieces, each the rounding of what the ones before it leave
+template <int N> __device__ __forceinline__ void split8(const float *y, bf16x8 *piece) {
+    float left[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) left[e] = y[e];
+#pragma unroll
+    for (int z = 0; z < N; ++z) {
+        u32x4 h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            h[e] = bf_pair(left[2 * e], left[2 * e + 1]);
+            left[2 * e] -= __uint_as_float(h[e] << 16);
+            left[2 * e + 1] -= __uint_as_float(h[e] & 0xFFFF0000u);
+        }
+        piece[z] = __builtin_bit_cast(bf16x8, h);
+    }
+}
+// eight codes of one block as a matrix operand
+__device__ __forceinline__ bf16x8 decode8(uint32_t c, float s) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1),
+                 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2), e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
+    const u32x4 r = {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, d),
+                     __builtin_bit_cast(uint32_t, e)};
+    return __builtin_bit_cast(bf16x8, r);
+}
+
+__device__ __forceinline__ f16x8 decode8h(uint32_t c, float s) {
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 1),
+                d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 3);
+    const u32x4 r = {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, d),
+                     __builtin_bit_cast(uint32_t, e)};
+    return __builtin_bit_cast(f16x8, r);
+}
+
+struct AttendArgs {
+    Pool p;
+    const int32_t *ctx_len;
+    const uint64_t *mask;
+    size_t mask_stride;
+    int batch, rows, n_heads, groups, max_len, wgs;
+    float scale;            // times log2(e)
+    const void *q;
+    size_t ldq;
+    void *out;
+    float *part, *ml;       // [wgs][2][MT * 16][DH] sums, [wgs][2][MT * 16][max, sum]
+};
+
+// keys of a sequence and the steps they are
+__device__ __forceinline__ int end_of(const AttendArgs &a, int b) { return max(0, min(max(a.ctx_len[b], 0) + a.rows, a.max_len)); }
+__device__ __forceinline__ int steps_of(int end) { return max(1, (end + STEP - 1) / STEP); }   // a sequence without keys has one too
+
+// The batch's steps laid end to end: lane j counts sequences j * per .. (j + 1) * per - 1
+struct Shares {
+    int before;      // steps of all items of the sequences before the lane's
+    int total, per;
+    int wgs;         // workgroups that have work: each of their waves a step at least, and an item's parts can be joined quickly
+    int q, r;        // workgroup w begins at step w * q + min(w, r)
+    __device__ __forceinline__ int first(int w) const { return w * q + min(w, r); }
+    __device__ __forceinline__ int owner(int step) const {   // the workgroup that takes a step
+        const int wide = r * (q + 1);
+        return step < wide ? step / (q + 1) : r + (step - wide) / q;
+    }
+};
+__device__ __forceinline__ Shares count_steps(const AttendArgs &a, int l) {
+    Shares s;
+    s.per = (a.batch + 63) / 64;
+    int mine = 0;
+    for (int i = 0; i < s.per; ++i) {
+        const int b = l * s.per + i;
+        if (b < a.batch) mine += steps_of(end_of(a, b));
+    }
+    const int items = a.p.n_kv * a.groups;
+    mine *= items;
+    // inclusive sums over the lanes: within rows of 16, then the rows' totals onto the rows after them
+    int x = mine;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, true);
+    s.before = x - mine;
+    s.total = __builtin_amdgcn_readlane(x, 63);
+    s.wgs = min(min(a.wgs, (s.total + WAVES - 1) / WAVES), items * a.batch * MAX_PARTS);
+    s.q = s.total / s.wgs;
+    s.r = s.total - s.q * s.wgs;
+    return s;
+}
+
+template <int DH, int MT, bool F32>
+__global__ __launch_bounds__(NT, 2) void k_paged_attend(AttendArgs a) {
+    constexpr int KS = DH / 32, DT = DH / 16, NQ = F32 ? 3 : 1;   // bfloat16 pieces of queries
+    constexpr int VS = DH * 2 + 32;        // bytes of a value row in LDS: a transposing load's 16 lanes hit different banks
+    constexpr int CW = DH / 32;            // 32-bit words of codes a lane takes of a key: a quarter of its dimensions
+    __shared__ __attribute__((aligned(16))) unsigned char vt_all[WAVES * STEP * VS];
+    __shared__ float mm[WAVES][16][2];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
+    unsigned char *vt = vt_all + wave * STEP * VS;
+
+    const Shares sh = count_steps(a, l);
+    // workgroups go to the eight dies in turn: neighbours in the work, which share keys, go to one die
+    const int n8 = sh.wgs & ~7;
+    const int w = (int)blockIdx.x < n8 ? ((int)blockIdx.x & 7) * (n8 >> 3) + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
+    if (w >= sh.wgs) return;
+    int at = sh.first(w);
+    const int end = sh.first(w + 1), begin = at;
+    // the sequence `at` lies in: the last lane whose share begins at or before it, then along that lane's sequences
+    const int lane = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64((sh.before <= at) & (l * sh.per < a.batch)));
+    int b = lane * sh.per, base = __builtin_amdgcn_readlane(sh.before, lane);
+    const int items = a.p.n_kv * a.groups;   // of a sequence
+    const int G = a.n_heads / a.p.n_kv;
+
+    while (at < end) {
+        const int kv_end = end_of(a, b), nsteps = steps_of(kv_end);
+        if (at - base >= items * nsteps) {
+            base += items * nsteps;
+            ++b;
+            continue;
+        }
+        const int item = (at - base) / nsteps, s0 = at - base - item * nsteps, n = min(nsteps - s0, end - at);
+        const int h = item / a.groups, row0 = (item - h * a.groups) * (MT * 16);
+        const int ctx = max(a.ctx_len[b], 0);
+        // ---- this item's queries and masks
+        bf16x8 qf[MT][KS][NQ];
+        uint64_t mask[MT];
+        unsigned nan_v[MT];   // quarters of the head whose values a row has seen that are not numbers
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int r = row0 + mt * 16 + li, t = r / G, g = r - t * G;
+            const bool ok = t < a.rows;
+            const size_t from = ((size_t)b * a.rows + (ok ? t : 0)) * a.ldq + (size_t)(h * G + g) * DH + lg * (DH / 4);
+            mask[mt] = !ok ? 0 : a.mask ? a.mask[b * a.mask_stride + t] : (2ull << t) - 1;
+            nan_v[mt] = 0;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if (F32) {
+                    float y[8];
+                    load8<true>(a.q, from + 8 * ks, y);
+                    split8<NQ>(y, qf[mt][ks]);
+                } else {
+                    qf[mt][ks][0] = __builtin_bit_cast(bf16x8, *(const u32x4 *)((const bf16_t *)a.q + from + 8 * ks));
+                }
+            }
+        }
+        f32x4 acc[MT][DT];
+        float m_run[MT], l_run[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            m_run[mt] = -INFINITY;
+            l_run[mt] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) acc[mt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+        // ---- the wave's steps: page numbers two steps ahead, codes one
+        const int32_t *table = a.p.table + (size_t)b * a.p.pages_per_seq;
+        const int last_key = max(kv_end - 1, 0), place = (1 << a.p.log_page) - 1;
+        uint32_t kc[2][CW], vc[2][CW];
+        unsigned ke[2], ve[2];
+        int page[2];
+        auto find = [&](int st) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) page[j] = table[min(st * STEP + 16 * j + li, last_key) >> a.p.log_page];
+        };
+        auto fetch = [&](int st) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int key = min(st * STEP + 16 * j + li, last_key);
+                // a page number outside the pool is the caller's mistake; it is kept from being an address outside of it
+                const unsigned pg = (unsigned)page[j] < (unsigned)a.p.n_pages ? (unsigned)page[j] : 0u;
+                const size_t r = (((size_t)pg * a.p.n_kv + h) << a.p.log_page) + (key & place);
+                const size_t o = r * (DH / 2) + lg * (4 * CW), e = r * (DH / BLOCK) + (DH == 128 ? lg : lg >> 1);
+                if (CW == 4) {
+                    *(u32x4 *)kc[j] = *(const u32x4 *)(a.p.k + o);
+                    *(u32x4 *)vc[j] = *(const u32x4 *)(a.p.v + o);
+                } else {
+                    *(u32x2 *)kc[j] = *(const u32x2 *)(a.p.k + o);
+                    *(u32x2 *)vc[j] = *(const u32x2 *)(a.p.v + o);
+                }
+                ke[j] = a.p.ks[e];
+                ve[j] = a.p.vs[e];
+            }
+        };
+        const int last = s0 + n;
+        if (s0 + wave < last) {
+            find(s0 + wave);
+            fetch(s0 + wave);
+            find(min(s0 + wave + WAVES, last - 1));
+        }
+        for (int st = s0 + wave; st < last; st += WAVES) {
+            const int k0 = st * STEP;
+            const bool full = k0 + STEP <= min(ctx, kv_end);   // every row sees all of the step's keys
+            uint32_t seen[MT];                                 // otherwise: which of them the lane's row sees
+            if (!full) {
+                const int d = k0 - ctx, left = kv_end - k0;    // the same for all lanes
+                const uint32_t there = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1 : 0u;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    seen[mt] = there & (d >= 64 ? 0u : d >= 0 ? (uint32_t)(mask[mt] >> d) : d > -32 ? (uint32_t)mask[mt] << -d | ((1u << -d) - 1) : ~0u);
+            }
+            // ---- S^T = K Q^T
+            f32x4 sc[2][MT];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) sc[j][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                const float s = ke[j] == NAN_EXP ? __builtin_nanf("") : exp_scale(ke[j]);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const bf16x8 kf = decode8(kc[j][ks], s);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int z = 0; z < NQ; ++z) sc[j][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][ks][z], sc[j][mt], 0, 0, 0);
+                }
+            }
+            // ---- values to LDS, as rows
+            bool half_v = false;   // as fp16, and probabilities too
+            if (!F32) half_v = __builtin_amdgcn_ballot_w64(((ve[0] - HALF_LO) > HALF_HI - HALF_LO) | ((ve[1] - HALF_LO) > HALF_HI - HALF_LO)) == 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float s = ve[j] == NAN_EXP ? __builtin_nanf("") : exp_scale(ve[j]);
+                uint32_t c[CW];
+#pragma unroll
+                for (int i = 0; i < CW; ++i) c[i] = vc[j][i];
+                if (!full) {
+                    // A slot past the end counts for nothing whatever it holds.  A value that is not a number is kept from the
+                    // rows that do not see it (0 times it would be one too): it is left out of the product here, and the rows
+                    // that do see it are marked.
+                    const bool in = k0 + 16 * j + li < kv_end;
+                    uint64_t bad = __builtin_amdgcn_ballot_w64(in & (ve[j] == NAN_EXP));
+                    while (bad != 0) {
+                        const int at_lane = __builtin_ctzll(bad);
+                        bad &= bad - 1;
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) nan_v[mt] |= ((seen[mt] >> (16 * j + (at_lane & 15))) & 1u) << (at_lane >> 4);
+                    }
+                    const bool drop = !in | (ve[j] == NAN_EXP);
+                    s = drop ? 1.f : s;
+#pragma unroll
+                    for (int i = 0; i < CW; ++i) c[i] = drop ? 0u : c[i];
+                }
+                unsigned char *to = vt + (16 * j + li) * VS + lg * (DH / 2);
+                if (half_v) {
+#pragma unroll
+                    for (int i = 0; i < CW; ++i) *(u32x4_alias *)(to + 16 * i) = __builtin_bit_cast(u32x4, decode8h(c[i], s));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < CW; ++i) *(u32x4_alias *)(to + 16 * i) = __builtin_bit_cast(u32x4, decode8(c[i], s));
+                }
+            }
+            if (st + WAVES < last) {
+                fetch(st + WAVES);
+                find(min(st + 2 * WAVES, last - 1));
+            }
+            // ---- mask, softmax in powers of two
+            // With M the largest score so far times `scale`, a weight is 2^(score * scale - M), one multiply-add and one power; for
+            // fp16 it is 2^8 of that, so that weights down to 2^-22 of the largest have all their bits.
+            float p[MT][8];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[mt][e] = sc[e >> 2][mt][e & 3];
+                if (!full) {   // selects, not branches: lanes differ
+                    const uint32_t mine = seen[mt] >> (4 * lg);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[mt][e] = (mine >> (16 * (e >> 2) + (e & 3))) & 1u ? p[mt][e] : -INFINITY;
+                }
+                float top = p[mt][0], sum = 0.f;
+#pragma unroll
+                for (int e = 1; e < 8; ++e) top = fmaxf(top, p[mt][e]);
+                const float m_new = fmaxf(m_run[mt], lane_groups_max(top) * a.scale);
+                // nothing seen so far: the weights below are 2^(-inf), not 2^(-inf + inf)
+                const float m_use = (m_new == -INFINITY ? 0.f : m_new) - (F32 ? 0.f : 8.f);
+                const float alpha = __builtin_amdgcn_exp2f(m_run[mt] - (m_new == -INFINITY ? 0.f : m_new));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    p[mt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[mt][e], a.scale, -m_use));
+                    sum += p[mt][e];
+                }
+                m_run[mt] = m_new;
+                l_run[mt] = l_run[mt] * alpha + sum;
+                if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) acc[mt][dt] *= alpha;
+                }
+            }
+            // ---- O^T += V^T P^T; slot (lane group g, element e) of the contraction is key 16 (e / 4) + 4 g + e % 4, which is
+            // where the scores lie.  Transposing load: lane i of 16 points at key row 4 g + i / 4, columns 16 dt + 4 (i % 4) ..
+            // and gets keys 4 g .. 4 g + 3 of column 16 dt + i.
+            const unsigned char *from = vt + (4 * lg + (li >> 2)) * VS + (li & 3) * 8;
+            auto values = [&](int dt) {
+                const bf16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(from + dt * 32));
+                const bf16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(from + dt * 32 + 16 * VS));
+                return __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
+            };
+            if (half_v) {
+                f16x8 ph[MT];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    ph[mt] = __builtin_convertvector((f32x8){p[mt][0], p[mt][1], p[mt][2], p[mt][3], p[mt][4], p[mt][5], p[mt][6], p[mt][7]}, f16x8);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    const f16x8 va = __builtin_bit_cast(f16x8, values(dt));
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) acc[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ph[mt], acc[mt][dt], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {   // tile by tile: the rare case needs few registers (one tile where it is the only one)
+                    bf16x8 pf[3];
+                    split8<3>(p[mt], pf);
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const bf16x8 va = values(dt);
+#pragma unroll
+                        for (int z = 0; z < 3; ++z) acc[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[z], acc[mt][dt], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        // ---- the waves meet, one row tile at a time; wave w then has DT / 4 of its 16-dimension pieces
+        const int which = at == begin ? 0 : 1;
+        const bool whole = n == nsteps;
+        f32x4_alias *mo = (f32x4_alias *)vt_all;   // [WAVES][DT][64]
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            if (__builtin_amdgcn_ballot_w64(nan_v[mt] != 0) != 0) {
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+                    if ((nan_v[mt] >> (dt * 64 / DH)) & 1)
+                        acc[mt][dt] = (f32x4){__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+            }
+            const float lsum = lane_groups_sum(l_run[mt]);
+            __syncthreads();
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) mo[(wave * DT + dt) * 64 + l] = acc[mt][dt];
+            if (lg == 0) {
+                mm[wave][li][0] = m_run[mt];
+                mm[wave][li][1] = lsum;
+            }
+            __syncthreads();
+            float M = -INFINITY, L = 0.f, f[WAVES];
+#pragma unroll
+            for (int v = 0; v < WAVES; ++v) M = fmaxf(M, mm[v][li][0]);
+            const float m_use = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int v = 0; v < WAVES; ++v) {
+                f[v] = __builtin_amdgcn_exp2f(mm[v][li][0] - m_use);
+                L += f[v] * mm[v][li][1];
+            }
+            const int r = row0 + mt * 16 + li, t = r / G, g = r - t * G;
+#pragma unroll
+            for (int i = 0; i < DT / WAVES; ++i) {
+                const int dt = wave * (DT / WAVES) + i;
+                f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int v = 0; v < WAVES; ++v) o += f[v] * (f32x4)mo[(v * DT + dt) * 64 + l];
+                if (t >= a.rows) continue;
+                if (whole) {
+                    o *= L == 0.f ? 0.f : 1.f / L;   // a row that sees nothing is zero
+                    const size_t to = (((size_t)b * a.rows + t) * a.n_heads + h * G + g) * DH + dt * 16 + 4 * lg;
+                    if (F32) *(f32x4 *)((float *)a.out + to) = o;
+                    else *(u32x2 *)((bf16_t *)a.out + to) = (u32x2){bf_pair(o[0], o[1]), bf_pair(o[2], o[3])};
+                } else {
+                    const size_t pr = ((size_t)w * 2 + which) * (MT * 16) + mt * 16 + li;
+                    *(f32x4 *)(a.part + pr * DH + dt * 16 + 4 * lg) = o;
+                    if (dt == 0 && lg == 0) {
+                        a.ml[pr * 2] = M;
+                        a.ml[pr * 2 + 1] = L;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        at += n;
+    }
+}
+
+// Joins the partial results of the items that more than one workgroup has worked on.  A workgroup an item and row tile, a lane
+// DH / 16 dimensions of a row.
+template <int DH, int MT, bool F32>
+__global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
+    constexpr int E = DH / 16;
+    const int l = threadIdx.x & 63;
+    const Shares sh = count_steps(a, l);
+    const int items = a.p.n_kv * a.groups;
+    const int item_ = blockIdx.x / MT, mt = blockIdx.x % MT, b = item_ / items, item = item_ - b * items;
+    const int nsteps = steps_of(end_of(a, b)), lane = b / sh.per;
+    int base = __builtin_amdgcn_readlane(sh.before, lane);
+    for (int i = lane * sh.per; i < b; ++i) base += items * steps_of(end_of(a, i));
+    const int from = base + item * nsteps, to = from + nsteps;
+    const int w0 = sh.owner(from), w1 = sh.owner(to - 1);
+    if (w0 == w1) return;   // one workgroup had all of it
+    const int G = a.n_heads / a.p.n_kv, h = item / a.groups;
+    const int li = threadIdx.x / 16, d0 = (threadIdx.x & 15) * E;
+    const int r = (item - h * a.groups) * (MT * 16) + mt * 16 + li, t = r / G, g = r - t * G;
+    if (t >= a.rows) return;
+    float M = -INFINITY, L = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int w = w0; w <= w1; ++w) {
+        const size_t pr = ((size_t)w * 2 + (sh.first(w) >= from ? 0 : 1)) * (MT * 16) + mt * 16 + li;
+        const float m = a.ml[pr * 2], ls = a.ml[pr * 2 + 1];
+        const float m_new = fmaxf(M, m), m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float fo = __builtin_amdgcn_exp2f(M - m_use), fn = __builtin_amdgcn_exp2f(m - m_use);
+        M = m_new;
+        L = L * fo + ls * fn;
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+            const f32x4 x = *(const f32x4 *)(a.part + pr * DH + d0 + e);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) o[e + z] = o[e + z] * fo + x[z] * fn;
+        }
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= inv;
+    const size_t at = (((size_t)b * a.rows + t) * a.n_heads + h * G + g) * DH + d0;
+    if (F32) {
+#pragma unroll
+        for (int e = 0; e < E; e += 4) *(f32x4 *)((float *)a.out + at + e) = (f32x4){o[e], o[e + 1], o[e + 2], o[e + 3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; e += 4) *(u32x2 *)((bf16_t *)a.out + at + e) = (u32x2){bf_pair(o[e], o[e + 1]), bf_pair(o[e + 2], o[e + 3])};
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+koala_status check_cache(const koala_paged_kv *kv, int batch) {
+    if (!kv || !kv->k || !kv->v || !kv->k_scale || !kv->v_scale || !kv->page_table || !kv->ctx_len) return KOALA_E_NULL;
+    if (kv->n_layers < 1 || kv->n_pages < 1 || kv->n_kv_heads < 1 || kv->n_kv_heads > 4096 || kv->pages_per_seq < 1 ||
+        kv->max_batch < 1 || batch < 1 || batch > kv->max_batch)
+        return KOALA_E_SHAPE;
+    if (kv->head_dim != 64 && kv->head_dim != 128) return KOALA_E_UNSUPPORTED;
+    const int p = kv->page_size;
+    if (p < 16 || p > 256 || (p & (p - 1))) return KOALA_E_UNSUPPORTED;
+    if ((long)kv->pages_per_seq * p > 0x7FFFFFFFl - 65536) return KOALA_E_SHAPE;
+    if (!aligned16(kv->k) || !aligned16(kv->v) || !aligned16(kv->k_scale) || !aligned16(kv->v_scale)) return KOALA_E_ALIGN;
+    return KOALA_OK;
+}
+Pool pool_of(const koala_paged_kv *kv, int layer) {
+    Pool p{};
+    p.n_pages = kv->n_pages;
+    p.log_page = __builtin_ctz((unsigned)kv->page_size);
+    p.n_kv = kv->n_kv_heads;
+    p.pages_per_seq = kv->pages_per_seq;
+    p.layer_rows = (size_t)kv->n_pages * kv->n_kv_heads * kv->page_size;
+    p.table = kv->page_table;
+    const size_t r = (size_t)layer * p.layer_rows;
+    p.k = (uint8_t *)kv->k + r * (kv->head_dim / 2);
+    p.v = (uint8_t *)kv->v + r * (kv->head_dim / 2);
+    p.ks = (uint8_t *)kv->k_scale + r * (kv->head_dim / BLOCK);
+    p.vs = (uint8_t *)kv->v_scale + r * (kv->head_dim / BLOCK);
+    return p;
+}
+koala_status launched() { return hipGetLastError() == hipSuccess ? KOALA_OK : KOALA_E_DEVICE; }
+// workgroups of 256 for n lanes; 0 if the lanes cannot be counted in 32 bits
+unsigned blocks_of(size_t n) { return n > 0xFFFFFF00ull ? 0 : (unsigned)((n + 255) / 256); }
+
+// row tiles of an attention item (the pieces of fp32 queries leave no registers for a second)
+int tiles_of(int rows, bool f32) { return rows <= 16 || f32 ? 1 : 2; }
+int attend_wgs(int cu) { return 2 * cu; }
+int compute_units() {
+    static const int n = [] {
+        int dev = 0, cu = 0;
+        if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 256;
+        return cu > 0 ? cu : 256;
+    }();
+    return n;
+}
+enum { ATTEND_WGS_MAX = 1024 };   // what the workspace is sized for
+
+template <int DH, int MT, bool F32>
+void launch_attend(hipStream_t st, const AttendArgs &a) {
+    k_paged_attend<DH, MT, F32><<<a.wgs, NT, 0, st>>>(a);
+    k_paged_join<DH, MT, F32><<<(unsigned)a.batch * a.p.n_kv * a.groups * MT, 256, 0, st>>>(a);
+}
+
+}  // namespace
+
+extern "C" {
+
+koala_status koala_paged_append(const koala_paged_kv *kv, void *hip_stream, int layer, int batch, int rows, int dtype, int n_heads,
+                                const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                                const int32_t *n_new, const int32_t *depth, const float *rope_cos, const float *rope_sin,
+                                int rope_rows, void *q_out) {
+    koala_status rc = check_cache(kv, batch);
+    if (rc != KOALA_OK) return rc;
+    if (!k || !v || !rope_cos || !rope_sin || (n_heads > 0 && (!q || !q_out))) return KOALA_E_NULL;
+    if (dtype != KOALA_FP32 && dtype != KOALA_BF16) return KOALA_E_UNSUPPORTED;
+    const int DH = kv->head_dim, KV = kv->n_kv_heads, unit = dtype == KOALA_FP32 ? 4 : 8;
+    if (layer < 0 || layer >= kv->n_layers || rows < 1 || n_heads < 0 || n_heads > 4096 || rope_rows < 1 || (long)batch * rows > 0x7FFFFFFFl)
+        return KOALA_E_SHAPE;
+    if (k_stride < (int64_t)KV * DH || v_stride < (int64_t)KV * DH || (n_heads > 0 && q_stride < (int64_t)n_heads * DH)) return KOALA_E_SHAPE;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(rope_cos) || !aligned16(rope_sin) || k_stride % unit || v_stride % unit ||
+        (n_heads > 0 && (!aligned16(q) || !aligned16(q_out) || q_stride % unit)))
+        return KOALA_E_ALIGN;
+    AppendArgs a{};
+    a.p = pool_of(kv, layer);
+    a.ctx_len = kv->ctx_len; a.n_new = n_new; a.depth = depth; a.cos = rope_cos; a.sin = rope_sin; a.rope_rows = rope_rows;
+    a.rows = batch * rows; a.rows_per_seq = rows; a.n_heads = n_heads;
+    a.q = q; a.k = k; a.v = v;
+    a.ldq = (size_t)q_stride; a.ldk = (size_t)k_stride; a.ldv = (size_t)v_stride;
+    a.q_out = q_out;
+    const unsigned g = blocks_of((size_t)a.rows * (n_heads + 2 * KV) * (DH / 16));
+    if (!g) return KOALA_E_SHAPE;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (DH == 128) {
+        if (dtype == KOALA_FP32) k_paged_append<128, true><<<g, 256, 0, st>>>(a);
+        else k_paged_append<128, false><<<g, 256, 0, st>>>(a);
+    } else {
+        if (dtype == KOALA_FP32) k_paged_append<64, true><<<g, 256, 0, st>>>(a);
+        else k_paged_append<64, false><<<g, 256, 0, st>>>(a);
+    }
+    return launched();
+}
+
+koala_status koala_paged_read(const koala_paged_kv *kv, void *hip_stream, int layer, int n_layers, int batch, const int32_t *start,
+                              int n, int dtype, void *k_out, void *v_out) {
+    koala_status rc = check_cache(kv, batch);
+    if (rc != KOALA_OK) return rc;
+    if (!k_out || !v_out) return KOALA_E_NULL;
+    if (dtype != KOALA_FP32 && dtype != KOALA_BF16) return KOALA_E_UNSUPPORTED;
+    if (layer < 0 || n_layers < 1 || layer > kv->n_layers - n_layers || n < 1) return KOALA_E_SHAPE;
+    if (!aligned16(k_out) || !aligned16(v_out)) return KOALA_E_ALIGN;
+    ReadArgs a{};
+    a.p = pool_of(kv, layer);
+    a.start = start; a.batch = (unsigned)batch; a.n = (unsigned)n; a.layers = (unsigned)n_layers; a.k_out = k_out; a.v_out = v_out;
+    const unsigned g = blocks_of((size_t)n_layers * batch * n * kv->n_kv_heads * (kv->head_dim / 8));
+    if (!g) return KOALA_E_SHAPE;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (kv->head_dim == 128) {
+        if (dtype == KOALA_FP32) k_paged_read<128, true><<<g, 256, 0, st>>>(a);
+        else k_paged_read<128, false><<<g, 256, 0, st>>>(a);
+    } else {
+        if (dtype == KOALA_FP32) k_paged_read<64, true><<<g, 256, 0, st>>>(a);
+        else k_paged_read<64, false><<<g, 256, 0, st>>>(a);
+    }
+    return launched();
+}
+
+koala_status koala_paged_commit(const koala_paged_kv *kv, void *hip_stream, int batch, const int32_t *accept_len,
+                                const int32_t *accept_path, int path_stride, int32_t *new_len) {
+    koala_status rc = check_cache(kv, batch);
+    if (rc != KOALA_OK) return rc;
+    if (!accept_len || !accept_path || !new_len) return KOALA_E_NULL;
+    if (path_stride < 1) return KOALA_E_SHAPE;
+    CommitArgs a{};
+    a.p = pool_of(kv, 0);
+    a.ctx_len = kv->ctx_len; a.accept_len = accept_len; a.accept_path = accept_path;
+    a.path_stride = path_stride; a.batch = (unsigned)batch; a.layers = (unsigned)kv->n_layers;
+    a.new_len = new_len == kv->ctx_len ? nullptr : new_len;
+    const unsigned g = blocks_of((size_t)kv->n_layers * batch * kv->n_kv_heads * (kv->head_dim / 16 + 2));
+    if (!g) return KOALA_E_SHAPE;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (kv->head_dim == 128) k_paged_commit<128><<<g, 256, 0, st>>>(a);
+    else k_paged_commit<64><<<g, 256, 0, st>>>(a);
+    // in place, the lengths may change only when no workgroup reads them any more
+    if (!a.new_len) k_paged_advance<<<(batch + 255) / 256, 256, 0, st>>>(kv->ctx_len, accept_len, batch);
+    return launched();
+}
+
+koala_status koala_paged_workspace_bytes(const koala_paged_kv *kv, size_t *out) {
+    if (!kv || !out) return KOALA_E_NULL;
+    if (kv->head_dim != 64 && kv->head_dim != 128) return KOALA_E_UNSUPPORTED;
+    *out = (size_t)ATTEND_WGS_MAX * 2 * 32 * (kv->head_dim + 2) * sizeof(float);
+    return KOALA_OK;
+}
+
+koala_status koala_paged_attend(const koala_paged_kv *kv, void *hip_stream, int layer, int batch, int rows, int dtype, int n_heads,
+                                const void *q, int64_t q_stride, const uint64_t *mask, int64_t mask_stride, float scale, int max_len,
+                                void *out, void *workspace, size_t workspace_bytes) {
+    koala_status rc = check_cache(kv, batch);
+    if (rc != KOALA_OK) return rc;
+    if (!q || !out || !workspace) return KOALA_E_NULL;
+    if (dtype != KOALA_FP32 && dtype != KOALA_BF16) return KOALA_E_UNSUPPORTED;
+    const int DH = kv->head_dim, KV = kv->n_kv_heads;
+    if (layer < 0 || layer >= kv->n_layers || rows < 1 || rows > KOALA_MAX_NODES || n_heads < 1 || n_heads > 4096 || n_heads % KV ||
+        q_stride < (int64_t)n_heads * DH || mask_stride < 0 || (mask && mask_stride > 0 && mask_stride < rows) || max_len < 0 || !(scale > 0.f) ||
+        !(scale < INFINITY))
+        return KOALA_E_SHAPE;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace) || q_stride % (dtype == KOALA_FP32 ? 4 : 8) || ((uintptr_t)mask & 7))
+        return KOALA_E_ALIGN;
+    size_t need = 0;
+    (void)koala_paged_workspace_bytes(kv, &need);
+    if (workspace_bytes < need) return KOALA_E_WORKSPACE;
+    const int MT = tiles_of(rows * (n_heads / KV), dtype == KOALA_FP32);
+    AttendArgs a{};
+    a.p = pool_of(kv, layer);
+    a.ctx_len = kv->ctx_len; a.mask = mask; a.mask_stride = (size_t)mask_stride;
+    a.batch = batch; a.rows = rows; a.n_heads = n_heads;
+    a.groups = (rows * (n_heads / KV) + MT * 16 - 1) / (MT * 16);
+    a.scale = scale * LOG2E;
+    const int room = kv->pages_per_seq * kv->page_size;
+    a.max_len = max_len > 0 && max_len < room ? max_len : room;
+    if ((double)batch * KV * a.groups * (a.max_len / STEP + 1) > 2147483647.0) return KOALA_E_SHAPE;   // steps are counted in 32 bits
+    a.wgs = attend_wgs(compute_units());
+    if (a.wgs > ATTEND_WGS_MAX) a.wgs = ATTEND_WGS_MAX;
+    a.q = q; a.ldq = (size_t)q_stride; a.out = out;
+    a.part = (float *)workspace;
+    a.ml = a.part + (size_t)a.wgs * 2 * MT * 16 * DH;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (DH == 128) {
+        if (dtype == KOALA_FP32) launch_attend<128, 1, true>(st, a);
+        else MT == 1 ? launch_attend<128, 1, false>(st, a) : launch_attend<128, 2, false>(st, a);
+    } else {
+        if (dtype == KOALA_FP32) launch_attend<64, 1, true>(st, a);
+        else MT == 1 ? launch_attend<64, 1, false>(st, a) : launch_attend<64, 2, false>(st, a);
+    }
+    return launched();
+}
+
+}  // extern "C"

@@ -94,3 +94,37 @@ def alloc_kv(cfg, max_batch, capacity, device="cuda", draft_layers=0):
         kv["draft_k"] = torch.zeros(dshp, dtype=td, device=device)
         kv["draft_v"] = torch.zeros(dshp, dtype=td, device=device)
     return kv
+
+
+def alloc_paged_cache(n_layers, n_pages, page_size, n_kv_heads, head_dim, device="cuda"):
+    """Pools of a 4-bit paged cache (see koala_paged_kv), not cleared: dict(k, v, k_scale, v_scale)."""
+    import torch
+    shp = (n_layers, n_pages, n_kv_heads, page_size)
+    pool = lambda n: torch.empty(*shp, n, dtype=torch.uint8, device=device)
+    return dict(k=pool(head_dim // 2), v=pool(head_dim // 2), k_scale=pool(head_dim // 32), v_scale=pool(head_dim // 32))
+
+
+def quantize_weight(w):
+    """A Linear weight [N, K] in 8 bits: int8 [N, K] and fp32 scales [N], the largest magnitude of an output channel at 127."""
+    import torch
+    w = w.float()
+    top = w.abs().amax(1)
+    scale = torch.where(top > 0, top / 127.0, torch.ones_like(top))
+    return (w / scale[:, None]).round().to(torch.int8), scale
+
+
+def rope_tables(positions, head_dim, base=10000.0, device="cuda"):
+    """cos and sin fp32 [positions, head_dim / 2] of the rotary embedding, computed in 64 bits."""
+    import torch
+    inv = base ** (-torch.arange(0, head_dim, 2, dtype=torch.float64, device=device) / head_dim)
+    angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * inv
+    return angle.cos().float(), angle.sin().float()
+
+
+def tree_masks(tree, device="cuda"):
+    """Which nodes every node of a tree sees, itself and its ancestors: int64 [n_nodes], bit j for node j."""
+    import torch
+    seen = []
+    for i, p in enumerate(int(v) for v in tree.parent):
+        seen.append((seen[p] if i else 0) | 1 << i)
+    return torch.tensor([m - (1 << 64) if m >= 1 << 63 else m for m in seen], dtype=torch.int64, device=device)
