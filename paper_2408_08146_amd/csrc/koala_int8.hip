@@ -1,6 +1,10 @@
 // Projections in 8-bit integers with a scale for each token and each output channel (koala.h, "Projections in 8-bit integers").
 #include "koala_internal.h"
+#include <stdlib.h>
 
+#ifndef KCS
+#define KCS 256
+#endif
 namespace {
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
@@ -11,6 +15,9 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 
 __device__ __forceinline__ float bf_lo(uint32_t p) { return __uint_as_float(p << 16); }
+__device__ __forceinline__ uint32_t bf_pair(float a, float b) {   // round to nearest even
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
+}
 __device__ __forceinline__ float bf_hi(uint32_t p) { return __uint_as_float(p & 0xFFFF0000u); }
 
 // ---------------------------------------------------------------------------------------------
@@ -172,6 +179,19 @@ __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
     if (tid == 0 && (nch & 1)) *(u32x2 *)(a.q + row * a.ldq + 8 * nch) = (u32x2){0u, 0u};
 }
 
+// Operands are read through buffer instructions: an address is one 32-bit offset a lane, and what lies outside the rows from `row` on
+// reads as zero.  (The whole offset is the lane's: the bounds check is of that one.)
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+constexpr unsigned OUTSIDE = 0x7FFFFFF0;   // an offset outside of any buffer, and whatever is added to it
+constexpr int STREAMED = 2;                // cache policy of what is read once
+__device__ __forceinline__ rsrc_t rows_from(const int8_t *p, size_t ld, int row, int rows, int cols) {
+    const size_t left = (size_t)(rows - 1 - row) * ld + cols;   // row < rows
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p + (size_t)row * ld), 0, left > 0x7FFFFF00ull ? 0x7FFFFF00 : (int)left, 0x00020000);
+}
+template <int AUX = 0> __device__ __forceinline__ i32x4 load16(rsrc_t r, unsigned lane, unsigned more) {
+    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(lane + more), 0, AUX));
+}
+
 // ---------------------------------------------------------------------------------------------
 // Products.  The matrix pipe multiplies 16 output channels by 16 rows over 64 terms: a lane holds 16 consecutive terms of one
 // channel or row, which is 16 bytes of the row-major matrix as it lies in memory.
@@ -183,78 +203,211 @@ struct LinearArgs {
     const void *add;
     void *y;
     int rows, out, in;
+    bool y_f32, vec;   // vec: rows of y (and add) begin on four elements
     int splits;
-    int *part;     // [splits][rows][out] where splits > 1
+    int *part;     // [splits][rows][out rounded up to 4] where splits > 1
 };
 
 // the four consecutive outputs n .. n + 3 of row m from their sums
-template <bool F32> __device__ __forceinline__ void finish4(const LinearArgs &a, int m, int n, i32x4 s) {
+__device__ __forceinline__ void finish4(const LinearArgs &a, int m, int n, i32x4 s) {
     if (m >= a.rows || n >= a.out) return;
     const float qs = a.q_scale[m];
     const size_t at = (size_t)m * a.ldy + n;
-    float v[4];
+    typedef float __attribute__((ext_vector_type(4), aligned(4))) f32x4_a4;
+    if (a.vec && n + 4 <= a.out) {
+        const f32x4 ws = *(const f32x4_a4 *)(a.w_scale + n);
+        f32x4 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = n + e < a.out ? (float)s[e] * qs * a.w_scale[n + e] : 0.f;
-    if (F32) {
-        const float *add = a.add ? (const float *)a.add + at : nullptr;
-        float *y = (float *)a.y + at;
+        for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * qs * ws[e];
+        if (a.y_f32) {
+            if (a.add) v += *(const f32x4 *)((const float *)a.add + at);
+            *(f32x4 *)((float *)a.y + at) = v;
+        } else {
+            if (a.add) {
+                const u32x2 d = *(const u32x2 *)((const bf16_t *)a.add + at);
+                v += (f32x4){bf_lo(d[0]), bf_hi(d[0]), bf_lo(d[1]), bf_hi(d[1])};
+            }
+            *(u32x2 *)((bf16_t *)a.y + at) = (u32x2){bf_pair(v[0], v[1]), bf_pair(v[2], v[3])};
+        }
+        return;
+    }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n + e < a.out) y[e] = v[e] + (add ? add[e] : 0.f);
-    } else {
-        const bf16_t *add = a.add ? (const bf16_t *)a.add + at : nullptr;
-        bf16_t *y = (bf16_t *)a.y + at;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n + e < a.out)
-                y[e] = (bf16_t)__builtin_bit_cast(uint16_t, (__bf16)(v[e] + (add ? bf_lo(add[e]) : 0.f)));
+    for (int e = 0; e < 4; ++e) {
+        if (n + e >= a.out) continue;
+        const float v = (float)s[e] * qs * a.w_scale[n + e];
+        if (a.y_f32) ((float *)a.y)[at + e] = v + (a.add ? ((const float *)a.add)[at + e] : 0.f);
+        else ((bf16_t *)a.y)[at + e] = (bf16_t)__builtin_bit_cast(uint16_t, (__bf16)(v + (a.add ? bf_lo(((const bf16_t *)a.add)[at + e]) : 0.f)));
     }
 }
 
-// Row groups: a workgroup owns 16 U output channels and MT row tiles, its waves take the 64-term steps in turn, both operands
-// straight from memory into registers, and meet in LDS.
-template <int U, int MT, int NW, bool F32>
-__global__ __launch_bounds__(64 * NW) void k_linear_rows(LinearArgs a) {
-    __shared__ i32x4 red[NW][U * MT][64];
+// Up to 64 rows: the weights stream.  A workgroup owns U groups of 16 output channels; its eight waves take chunks of KC terms in turn.  A
+// wave asks memory for whole runs of a channel or row, KC bytes at a time: reading an operand as the matrix pipe wants it, 64 bytes of
+// 16 channels an instruction, streams 4.4 to 5.1 TB/s here, runs of 1 KiB 6.2.  It turns a tile (16 rows or channels of a chunk) into
+// operands through LDS of its own (no barrier; 16-byte pieces at their place XOR the row's number).  A chunk is MT tiles of the rows,
+// kept as operands, and U of the weights; AHEAD tiles are under way in registers.
+template <int U, int MT, int KC, int AHEAD>
+__global__ __launch_bounds__(512) void k_linear_rows(LinearArgs a) {
+    constexpr int NW = 8, KS = KC / 64, LD = KC / 64, V = U + MT;   // LD: loads a tile is
+    constexpr int LPR = KC / 16, RPL = 64 / LPR;                    // lanes of a run, runs of a load
+    constexpr size_t TURN = (size_t)NW * 16 * KC, RED = (size_t)(NW / 2) * U * MT * 1024;
+    static_assert(V % AHEAD == 0, "a tile's registers are the same in every chunk");
+    __shared__ __attribute__((aligned(16))) int8_t lds[TURN > RED ? TURN : RED];
+    i32x4(*red)[U * MT][64] = (i32x4(*)[U * MT][64])lds;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
+    int8_t *mine = lds + wave * (16 * KC);
     const int n0 = blockIdx.x * (16 * U), m0 = blockIdx.y * (16 * MT);
-    const int8_t *wp[U], *xp[MT];
-#pragma unroll
-    for (int u = 0; u < U; ++u) wp[u] = a.w + (size_t)min(n0 + 16 * u + li, a.out - 1) * a.ldw;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) xp[m] = a.q + (size_t)min(m0 + 16 * m + li, a.rows - 1) * a.ldq;
+    const int lr = l / LPR, lp = l % LPR, ldw = (int)a.ldw, ldq = (int)a.ldq;
+    const rsrc_t wr = rows_from(a.w, a.ldw, n0, a.out, a.in), xr = rows_from(a.q, a.ldq, m0, a.rows, a.in);
+    const unsigned w_lane = lr * ldw + 16 * lp, x_lane = lr * ldq + 16 * lp;
     i32x4 acc[U][MT];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[u][m] = (i32x4){0, 0, 0, 0};
-    for (int k0 = wave * 64; k0 < a.in; k0 += NW * 64) {
-        const int k = k0 + 16 * lg;
-        const bool in = k < a.in;         // past the end: any weights, times zero
-        const int kk = in ? k : 0;
-        i32x4 x[MT];
+    const int chunks = (a.in + KC - 1) / KC;
+    i32x4 t[AHEAD][LD], x[KS][MT];
+    // tile v of chunk c: past the last chunk nothing; past a row's end zeros for the rows, whatever there is for the weights
+    auto load = [&](int c, int v) {
+        if (v < MT) {
+            const unsigned at = c * KC + 16 * lp < a.in ? x_lane + c * KC : OUTSIDE;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            x[m] = *(const i32x4 *)(xp[m] + kk);
-            if (!in) x[m] = (i32x4){0, 0, 0, 0};
+            for (int i = 0; i < LD; ++i) t[v % AHEAD][i] = load16(xr, at, (16 * v + RPL * i) * ldq);
+        } else {
+            const unsigned at = c < chunks ? w_lane + c * KC : OUTSIDE;
+#pragma unroll
+            for (int i = 0; i < LD; ++i) t[v % AHEAD][i] = load16<STREAMED>(wr, at, (16 * (v - MT) + RPL * i) * ldw);
         }
+    };
+    if (wave < chunks) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const i32x4 w = *(const i32x4 *)(wp[u] + kk);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) acc[u][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x[m], acc[u][m], 0, 0, 0);
-        }
+        for (int v = 0; v < AHEAD; ++v) load(wave, v);
     }
+    for (int c = wave; c < chunks; c += NW)
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+        for (int v = 0; v < V; ++v) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) red[wave][u * MT + m][l] = acc[u][m];
+            for (int i = 0; i < LD; ++i) {
+                const int r = RPL * i + lr;
+                *(i32x4 *)(mine + r * KC + ((lp ^ (r & 15)) << 4)) = t[v % AHEAD][i];
+            }
+            if (v + AHEAD < V) load(c, v + AHEAD);
+            else load(c + NW, v + AHEAD - V);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const i32x4 o = *(const i32x4 *)(mine + li * KC + (((4 * s + lg) ^ li) << 4));
+                if (v < MT) x[s][v < MT ? v : 0] = o;
+                else
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+                        acc[v < MT ? 0 : v - MT][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o, x[s][m], acc[v < MT ? 0 : v - MT][m], 0, 0, 0);
+            }
+        }
     __syncthreads();
+    // the waves' sums, the upper four onto the lower four, then these
+#pragma unroll
+    for (int half = 1; half >= 0; --half) {
+        if ((wave >> 2) == half)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    if (half == 0) acc[u][m] += red[wave][u * MT + m][l];
+                    red[wave & 3][u * MT + m][l] = acc[u][m];
+                }
+        __syncthreads();
+    }
     for (int p = wave; p < U * MT; p += NW) {
         i32x4 s = red[0][p][l];
-        for (int v = 1; v < NW; ++v) s += red[v][p][l];
-        finish4<F32>(a, m0 + 16 * (p % MT) + li, n0 + 16 * (p / MT) + 4 * lg, s);
+#pragma unroll
+        for (int v = 1; v < NW / 2; ++v) s += red[v][p][l];
+        finish4(a, m0 + 16 * (p % MT) + li, n0 + 16 * (p / MT) + 4 * lg, s);
     }
+}
+
+// More rows: tiles of BM rows by BN channels through LDS, four waves of 16 TM rows by 16 TN channels each; 128 terms at a time, the next
+// ones on their way into registers while these are multiplied.  A row's 16-byte pieces are stored at their place XOR the row's number
+// modulo 8: a wave's reads of 16 rows then meet different banks.
+template <int TM, int TN>
+__global__ __launch_bounds__(256) void k_linear_tiles(LinearArgs a) {
+    constexpr int BM = 32 * TM, BN = 32 * TN, LX = BM / 32, LW = BN / 32;   // 16-byte loads a thread
+    __shared__ __attribute__((aligned(16))) int8_t sx[2][BM * 128], sw[2][BN * 128];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
+    const int nm = (a.rows + BM - 1) / BM, nn = (a.out + BN - 1) / BN, total = nm * nn * a.splits;
+    // neighbours in the work share weights: they go to one die (workgroups go to the eight dies in turn)
+    int t = (int)blockIdx.x;
+    const int per = total >> 3;
+    if (t < per * 8) t = (t & 7) * per + (t >> 3);
+    const int sp = t / (nm * nn), m0 = (t % (nm * nn)) % nm * BM, n0 = (t % (nm * nn)) / nm * BN;
+    const int chunks = (a.in + 127) / 128, c0 = chunks * sp / a.splits, c1 = chunks * (sp + 1) / a.splits;
+    const int row = tid >> 3, piece = tid & 7, put = row * 128 + ((piece ^ (row & 7)) << 4);
+    const int ldw = (int)a.ldw, ldq = (int)a.ldq;
+    const rsrc_t wr = rows_from(a.w, a.ldw, n0, a.out, a.in), xr = rows_from(a.q, a.ldq, m0, a.rows, a.in);
+    const unsigned w_lane = row * ldw + 16 * piece, x_lane = row * ldq + 16 * piece;
+    i32x4 rx[LX], rw[LW];
+    auto load = [&](int c) {   // past a row's end: any weights, times zero
+        const int k = c * 128;
+        const unsigned at = k + 16 * piece < a.in ? x_lane : OUTSIDE;
+#pragma unroll
+        for (int i = 0; i < LX; ++i) rx[i] = load16(xr, at, 32 * i * ldq + k);
+#pragma unroll
+        for (int i = 0; i < LW; ++i) rw[i] = load16(wr, w_lane, 32 * i * ldw + k);
+    };
+    auto store = [&](int slot) {
+#pragma unroll
+        for (int i = 0; i < LX; ++i) *(i32x4 *)(sx[slot] + put + 32 * 128 * i) = rx[i];
+#pragma unroll
+        for (int i = 0; i < LW; ++i) *(i32x4 *)(sw[slot] + put + 32 * 128 * i) = rw[i];
+    };
+    i32x4 acc[TN][TM];
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int m = 0; m < TM; ++m) acc[n][m] = (i32x4){0, 0, 0, 0};
+    const int wm = (wave & 1) * 16 * TM, wn = (wave >> 1) * 16 * TN;
+    if (c0 < c1) {
+        load(c0);
+        store(0);
+    }
+    __syncthreads();
+    for (int c = c0; c < c1; ++c) {
+        const int slot = (c - c0) & 1;
+        if (c + 1 < c1) load(c + 1);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int at = ((4 * s + lg) ^ (li & 7)) << 4;
+            i32x4 x[TM], w[TN];
+#pragma unroll
+            for (int m = 0; m < TM; ++m) x[m] = *(const i32x4 *)(sx[slot] + (wm + 16 * m + li) * 128 + at);
+#pragma unroll
+            for (int n = 0; n < TN; ++n) w[n] = *(const i32x4 *)(sw[slot] + (wn + 16 * n + li) * 128 + at);
+#pragma unroll
+            for (int n = 0; n < TN; ++n)
+#pragma unroll
+                for (int m = 0; m < TM; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[n], x[m], acc[n][m], 0, 0, 0);
+        }
+        if (c + 1 < c1) store(slot ^ 1);
+        __syncthreads();
+    }
+    const int ldp = (a.out + 3) / 4 * 4;
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int m = 0; m < TM; ++m) {
+            const int row_ = m0 + wm + 16 * m + li, col = n0 + wn + 16 * n + 4 * lg;
+            if (a.splits == 1) finish4(a, row_, col, acc[n][m]);
+            else if (row_ < a.rows && col < a.out) *(i32x4 *)(a.part + ((size_t)sp * a.rows + row_) * ldp + col) = acc[n][m];
+        }
+}
+
+// Sums of the splits, and the outputs: four a thread
+__global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
+    const unsigned quads = (a.out + 3) / 4, at = blockIdx.x * 256 + threadIdx.x, row = at / quads, quad = at - row * quads;
+    if (row >= (unsigned)a.rows) return;
+    const size_t stride = (size_t)a.rows * quads;
+    const i32x4 *p = (const i32x4 *)a.part + (size_t)row * quads + quad;
+    i32x4 s = p[0];
+    for (int i = 1; i < a.splits; ++i) s += p[i * stride];
+    finish4(a, row, 4 * quad, s);
 }
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
@@ -267,6 +420,62 @@ template <int FORM, bool F32> void quantize(hipStream_t st, const QuantArgs &a, 
     else if (nch <= 2 * threads) k_quantize_rows<FORM, F32, 2><<<rows, threads, 0, st>>>(a);
     else if (nch <= 4 * threads) k_quantize_rows<FORM, F32, 4><<<rows, threads, 0, st>>>(a);
     else k_quantize_rows<FORM, F32, 0><<<rows, threads, 0, st>>>(a);
+}
+
+struct Plan {
+    int tile;     // 0: row groups; else the tiles' form
+    int units;    // row groups: groups of 16 channels a workgroup
+    int splits;
+};
+Plan plan_of(int rows, int out, int in) {
+    Plan p{0, 1, 1};
+    if (rows <= 64) {
+        const int groups = (out + 15) / 16;
+        int best = 0x7FFFFFFF;
+        for (int u : {1, 2, 3, 4, 6, 8}) {
+            if (u == 8 && rows > 32) continue;
+            const int wgs = (groups + u - 1) / u, cost = (wgs + 255) / 256 * (u + 1);
+            if (cost <= best) {
+                best = cost;
+                p.units = u;
+            }
+        }
+        return p;
+    }
+    const char *e = getenv("TILE"), *sp = getenv("SPL");
+    p.tile = e ? atoi(e) : 1;
+    p.splits = sp ? atoi(sp) : 1;
+    return p;
+}
+
+template <int U, int MT, int KC, int AHEAD> void rows_launch(hipStream_t st, const LinearArgs &a) {
+    k_linear_rows<U, MT, KC, AHEAD><<<dim3((a.out + 16 * U - 1) / (16 * U), (a.rows + 16 * MT - 1) / (16 * MT)), 512, 0, st>>>(a);
+}
+template <int MT> void rows_by_units(hipStream_t st, const LinearArgs &a, int units) {
+    switch (units) {
+    case 1: rows_launch<1, MT, MT == 4 ? 256 : KCS, 1 + MT>(st, a); break;
+    case 2: rows_launch<2, MT, MT == 4 ? 256 : KCS, MT == 1 ? 3 : MT == 2 ? 4 : 3>(st, a); break;
+    case 3: rows_launch<3, MT, 256, MT == 1 ? 4 : MT == 2 ? 5 : 7>(st, a); break;
+    case 4: rows_launch<4, MT, 256, MT == 1 ? 5 : MT == 2 ? 6 : 4>(st, a); break;
+    case 6: rows_launch<6, MT, 256, MT == 1 ? 7 : MT == 2 ? 4 : 5>(st, a); break;
+    default: if constexpr (MT < 4) rows_launch<8, MT, 256, MT == 1 ? 3 : 5>(st, a); break;
+    }
+}
+template <int TM, int TN> void tiles_launch(hipStream_t st, const LinearArgs &a) {
+    k_linear_tiles<TM, TN><<<(a.rows + 32 * TM - 1) / (32 * TM) * ((a.out + 32 * TN - 1) / (32 * TN)) * a.splits, 256, 0, st>>>(a);
+}
+void launch_linear(hipStream_t st, const LinearArgs &a, const Plan &p) {
+    switch (p.tile) {
+    case 0:
+        if (a.rows <= 16) rows_by_units<1>(st, a, p.units);
+        else if (a.rows <= 32) rows_by_units<2>(st, a, p.units);
+        else rows_by_units<4>(st, a, p.units);
+        return;
+    case 1: tiles_launch<4, 4>(st, a); break;
+    case 2: tiles_launch<8, 4>(st, a); break;
+    case 3: tiles_launch<4, 8>(st, a); break;
+    }
+    if (a.splits > 1) k_linear_join<<<(unsigned)(((size_t)a.rows * ((a.out + 3) / 4) + 255) / 256), 256, 0, st>>>(a);
 }
 
 }  // namespace
@@ -299,7 +508,8 @@ koala_status koala_quantize_rows(void *hip_stream, int form, int x_dtype, int ro
 koala_status koala_linear_workspace_bytes(int rows, int out_features, int in_features, size_t *out) {
     if (!out) return KOALA_E_NULL;
     if (rows < 1 || out_features < 1 || in_features < 16 || in_features % 16 || in_features > 131056) return KOALA_E_SHAPE;
-    *out = 0;
+    const Plan p = plan_of(rows, out_features, in_features);
+    *out = p.splits > 1 ? (size_t)p.splits * rows * ((out_features + 3) / 4) * 16 : 0;
     return KOALA_OK;
 }
 
@@ -312,16 +522,18 @@ koala_status koala_linear_quantized(void *hip_stream, int rows, int out_features
     const koala_status rc = koala_linear_workspace_bytes(rows, out_features, in_features, &need);
     if (rc != KOALA_OK) return rc;
     if (q_stride < in_features || w_stride < in_features || y_stride < out_features) return KOALA_E_SHAPE;
+    const uintptr_t unit = y_dtype == KOALA_FP32 ? 4 : 2;
     if (!aligned16(q) || !aligned16(w) || q_stride % 16 || w_stride % 16 || !aligned16(workspace) || ((uintptr_t)q_scale & 3) || ((uintptr_t)w_scale & 3) ||
-        ((uintptr_t)y & (y_dtype == KOALA_FP32 ? 3 : 1)) || ((uintptr_t)add & (y_dtype == KOALA_FP32 ? 3 : 1)))
+        (uintptr_t)y % unit || (uintptr_t)add % unit)
         return KOALA_E_ALIGN;
+    if (q_stride > (1 << 22) || w_stride > (1 << 22)) return KOALA_E_SHAPE;   // 256 rows' bytes are counted in 31 bits
     if (need > 0 && (!workspace || workspace_bytes < need)) return KOALA_E_WORKSPACE;
-    LinearArgs a{q, w, (size_t)q_stride, (size_t)w_stride, (size_t)y_stride, q_scale, w_scale, add, y, rows, out_features, in_features, 1, (int *)workspace};
+    const Plan p = plan_of(rows, out_features, in_features);
+    const bool vec = y_stride % 4 == 0 && (uintptr_t)y % (4 * unit) == 0 && (uintptr_t)add % (4 * unit) == 0;
+    LinearArgs a{q, w, (size_t)q_stride, (size_t)w_stride, (size_t)y_stride, q_scale, w_scale, add, y, rows, out_features, in_features, y_dtype == KOALA_FP32, vec,
+                 p.splits, (int *)workspace};
     hipStream_t st = (hipStream_t)hip_stream;
-    const dim3 g((out_features + 31) / 32, (rows + 63) / 64);
-    if (g.y > 65535) return KOALA_E_SHAPE;
-    if (y_dtype == KOALA_FP32) k_linear_rows<2, 4, 4, true><<<g, 256, 0, st>>>(a);
-    else k_linear_rows<2, 4, 4, false><<<g, 256, 0, st>>>(a);
+    launch_linear(st, a, p);
     return launched();
 }
 

@@ -263,21 +263,23 @@ __global__ void k_paged_advance(int32_t *len, const int32_t *accept_len, int bat
 // The work is the items' steps of 32 keys laid end to end, and workgroup w of `wgs` takes [w * total / wgs, (w + 1) * total / wgs):
 // every compute unit gets the same number of keys whatever the sequences' lengths, which only the device knows.  An item that one
 // workgroup has taken whole is finished there; of the others each workgroup leaves a partial result (at most two a workgroup),
-// and a second launch joins them.  Within a workgroup four waves take the steps in turn and meet in LDS at the item's end.
+// and a second launch joins them.  Within a workgroup the waves take the steps in turn and meet in LDS at the item's end.
 //
 // A step of a wave: S^T[key][row] = K Q^T on the matrix pipe (a lane's 16 bytes of codes are 32 dimensions of a key: the
 // contraction's order over the head dimension is chosen so that they are four operands as they lie), softmax in powers of two,
 // O^T += V^T P^T with V converted to 16 bits, put into LDS as rows and read back through the transposing load.  For bfloat16
-// outputs P and V are fp16: V is exact as long as its exponents are (which a wave asks of every step), P has 11 bits, an eighth of
-// the output's own rounding.  For fp32 outputs, and for the steps whose values leave fp16's range, V is bfloat16, exact always, and P the
-// sum of three bfloat16 pieces; so are fp32 queries.  bfloat16 queries are exact.
+// outputs P and V are fp16: V is exact as long as its exponents are in range (a wave that meets one that is not does its steps again the
+// other way), P has 11 bits, an eighth of the output's own rounding.  For fp32 outputs, and where rows differ in what they see, V is
+// bfloat16, exact always, and P the sum of three bfloat16 pieces; so are fp32 queries.  bfloat16 queries are exact.
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 typedef u32x4 __attribute__((may_alias)) u32x4_alias;
 typedef f32x4 __attribute__((may_alias)) f32x4_alias;
 typedef float __attribute__((may_alias)) f32_alias;
 
-constexpr int WAVES = 4, NT = 64 * WAVES, STEP = 32;
+constexpr int WAVES = 4, STEP = 32;   // of a workgroup that shares items with others
+// An item counts for so many steps more where the work is divided: its first codes' way, the waves' meeting.
+constexpr int PER_ITEM = 24;
 constexpr int MAX_PARTS = 32;   // workgroups an item is spread over, on average at most
 constexpr float LOG2E = 1.44269504088896340736f;
 // block exponents (plus 127) whose values fp16 holds exactly: 1/2 2^-23 is its smallest, 6 2^13 below its largest
@@ -321,6 +323,13 @@ __device__ __forceinline__ bf16x8 decode8(uint32_t c, float s) {
     return __builtin_bit_cast(bf16x8, r);
 }
 
+template <int N> using words = __attribute__((ext_vector_type(N))) unsigned int;
+// what a lane holds of a step: a quarter of the head of two keys and their values, and the exponents
+template <int CW> struct Codes {
+    words<CW> k[2], v[2];
+    unsigned ke[2], ve[2];
+};
+__device__ __forceinline__ float block_scale(unsigned e) { return e == NAN_EXP ? __builtin_nanf("") : exp_scale(e); }
 __device__ __forceinline__ f16x8 decode8h(uint32_t c, float s) {
     const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 1),
                 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 3);
@@ -346,7 +355,7 @@ struct AttendArgs {
 __device__ __forceinline__ int end_of(const AttendArgs &a, int b) { return max(0, min(max(a.ctx_len[b], 0) + a.rows, a.max_len)); }
 __device__ __forceinline__ int steps_of(int end) { return max(1, (end + STEP - 1) / STEP); }   // a sequence without keys has one too
 
-// The batch's steps laid end to end: lane j counts sequences j * per .. (j + 1) * per - 1
+// The batch's items laid end to end, an item being its steps and PER_ITEM more: lane j counts sequences j * per .. (j + 1) * per - 1
 struct Shares {
     int before;      // steps of all items of the sequences before the lane's
     int total, per;
@@ -364,7 +373,7 @@ __device__ __forceinline__ Shares count_steps(const AttendArgs &a, int l) {
     int mine = 0;
     for (int i = 0; i < s.per; ++i) {
         const int b = l * s.per + i;
-        if (b < a.batch) mine += steps_of(end_of(a, b));
+        if (b < a.batch) mine += steps_of(end_of(a, b)) + PER_ITEM;
     }
     const int items = a.p.n_kv * a.groups;
     mine *= items;
@@ -384,41 +393,65 @@ __device__ __forceinline__ Shares count_steps(const AttendArgs &a, int l) {
     return s;
 }
 
-template <int DH, int MT, bool F32>
-__global__ __launch_bounds__(NT, 2) void k_paged_attend(AttendArgs a) {
+// Steps whose codes a wave has under way besides the one it works on
+constexpr int ahead(int MT, bool F32) { return MT == 2 ? 3 : F32 ? 2 : 3; }
+
+// WHOLE: every item is one workgroup's, of eight waves; the grid is the items
+template <int DH, int MT, bool F32, bool WHOLE>
+__global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, MT == 2 || F32 || WHOLE ? 2 : 3) void k_paged_attend(AttendArgs a) {
+    constexpr int NW = WHOLE ? 8 : WAVES;
     constexpr int KS = DH / 32, DT = DH / 16, NQ = F32 ? 3 : 1;   // bfloat16 pieces of queries
     constexpr int VS = DH * 2 + 32;        // bytes of a value row in LDS: a transposing load's 16 lanes hit different banks
     constexpr int CW = DH / 32;            // 32-bit words of codes a lane takes of a key: a quarter of its dimensions
-    __shared__ __attribute__((aligned(16))) unsigned char vt_all[WAVES * STEP * VS];
-    __shared__ float mm[WAVES][16][2];
+    __shared__ __attribute__((aligned(16))) unsigned char vt_all[NW * STEP * VS];
+    __shared__ float mm[NW][16][2];
+    constexpr bool QLDS = MT == 2;         // two tiles' queries are kept in LDS: the registers hold codes instead
+    __shared__ u32x4 qs[QLDS ? MT * KS * 64 : 1];
+    constexpr int AHEAD = ahead(MT, F32);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
     unsigned char *vt = vt_all + wave * STEP * VS;
 
-    const Shares sh = count_steps(a, l);
-    // workgroups go to the eight dies in turn: neighbours in the work, which share keys, go to one die
-    const int n8 = sh.wgs & ~7;
-    const int w = (int)blockIdx.x < n8 ? ((int)blockIdx.x & 7) * (n8 >> 3) + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
-    if (w >= sh.wgs) return;
-    int at = sh.first(w);
-    const int end = sh.first(w + 1), begin = at;
-    // the sequence `at` lies in: the last lane whose share begins at or before it, then along that lane's sequences
-    const int lane = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64((sh.before <= at) & (l * sh.per < a.batch)));
-    int b = lane * sh.per, base = __builtin_amdgcn_readlane(sh.before, lane);
     const int items = a.p.n_kv * a.groups;   // of a sequence
     const int G = a.n_heads / a.p.n_kv;
+    int w = (int)blockIdx.x, b = 0, base = 0, at = 0, end = 1, begin = 0;
+    if (WHOLE) {
+        b = w / items;
+    } else {
+        const Shares sh = count_steps(a, l);
+        // workgroups go to the eight dies in turn: neighbours in the work, which share keys, go to one die
+        const int n8 = sh.wgs & ~7;
+        if (w < n8) w = (w & 7) * (n8 >> 3) + (w >> 3);
+        if (w >= sh.wgs) return;
+        at = begin = sh.first(w);
+        end = sh.first(w + 1);
+        // the sequence `at` lies in: the last lane whose share begins at or before it, then along that lane's sequences
+        const int lane = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64((sh.before <= at) & (l * sh.per < a.batch)));
+        b = lane * sh.per;
+        base = __builtin_amdgcn_readlane(sh.before, lane);
+    }
 
     while (at < end) {
-        const int kv_end = end_of(a, b), nsteps = steps_of(kv_end);
-        if (at - base >= items * nsteps) {
-            base += items * nsteps;
-            ++b;
-            continue;
+        const int kv_end = end_of(a, b), nsteps = steps_of(kv_end), span = nsteps + PER_ITEM;
+        int item = w - b * items, s0 = 0, part = 1, n = nsteps;
+        if (!WHOLE) {
+            if (at - base >= items * span) {
+                base += items * span;
+                ++b;
+                continue;
+            }
+            item = (at - base) / span;
+            s0 = at - base - item * span;
+            part = min(span - s0, end - at);
+            n = min(s0 + part, nsteps) - s0;
+            if (n <= 0) {   // no step of the item is in this workgroup's share
+                at += part;
+                continue;
+            }
         }
-        const int item = (at - base) / nsteps, s0 = at - base - item * nsteps, n = min(nsteps - s0, end - at);
         const int h = item / a.groups, row0 = (item - h * a.groups) * (MT * 16);
         const int ctx = max(a.ctx_len[b], 0);
         // ---- this item's queries and masks
-        bf16x8 qf[MT][KS][NQ];
+        bf16x8 qf[QLDS ? 1 : MT][KS][NQ];
         uint64_t mask[MT];
         unsigned nan_v[MT];   // quarters of the head whose values a row has seen that are not numbers
 #pragma unroll
@@ -433,192 +466,213 @@ __global__ __launch_bounds__(NT, 2) void k_paged_attend(AttendArgs a) {
                 if (F32) {
                     float y[8];
                     load8<true>(a.q, from + 8 * ks, y);
-                    split8<NQ>(y, qf[mt][ks]);
-                } else {
-                    qf[mt][ks][0] = __builtin_bit_cast(bf16x8, *(const u32x4 *)((const bf16_t *)a.q + from + 8 * ks));
+                    split8<NQ>(y, qf[QLDS ? 0 : mt][ks]);
+                } else if (!QLDS) {
+                    qf[QLDS ? 0 : mt][ks][0] = __builtin_bit_cast(bf16x8, *(const u32x4 *)((const bf16_t *)a.q + from + 8 * ks));
+                } else if ((mt * KS + ks) % NW == wave) {
+                    qs[(mt * KS + ks) * 64 + l] = *(const u32x4 *)((const bf16_t *)a.q + from + 8 * ks);
                 }
             }
         }
+        if (QLDS) __syncthreads();
         f32x4 acc[MT][DT];
         float m_run[MT], l_run[MT];
+        auto reset = [&]() {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            m_run[mt] = -INFINITY;
-            l_run[mt] = 0.f;
+            for (int mt = 0; mt < MT; ++mt) {
+                m_run[mt] = -INFINITY;
+                l_run[mt] = 0.f;
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) acc[mt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        }
-        // ---- the wave's steps: page numbers two steps ahead, codes one
-        const int32_t *table = a.p.table + (size_t)b * a.p.pages_per_seq;
-        const int last_key = max(kv_end - 1, 0), place = (1 << a.p.log_page) - 1;
-        uint32_t kc[2][CW], vc[2][CW];
-        unsigned ke[2], ve[2];
-        int page[2];
-        auto find = [&](int st) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) page[j] = table[min(st * STEP + 16 * j + li, last_key) >> a.p.log_page];
+                for (int dt = 0; dt < DT; ++dt) acc[mt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            }
         };
-        auto fetch = [&](int st) {
+        reset();
+        const int32_t *table = a.p.table + (size_t)b * a.p.pages_per_seq;
+        const int last_key = max(kv_end - 1, 0), place = (1 << a.p.log_page) - 1, last = s0 + n;
+        // the wave's steps are s0 + wave + NW * i; steps past the last one are asked for as the last
+        auto find = [&](int *page, int st) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) page[j] = table[min(min(st, last - 1) * STEP + 16 * j + li, last_key) >> a.p.log_page];
+        };
+        auto fetch = [&](Codes<CW> &c, const int *page, int st) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int key = min(st * STEP + 16 * j + li, last_key);
+                const int key = min(min(st, last - 1) * STEP + 16 * j + li, last_key);
                 // a page number outside the pool is the caller's mistake; it is kept from being an address outside of it
                 const unsigned pg = (unsigned)page[j] < (unsigned)a.p.n_pages ? (unsigned)page[j] : 0u;
                 const size_t r = (((size_t)pg * a.p.n_kv + h) << a.p.log_page) + (key & place);
                 const size_t o = r * (DH / 2) + lg * (4 * CW), e = r * (DH / BLOCK) + (DH == 128 ? lg : lg >> 1);
-                if (CW == 4) {
-                    *(u32x4 *)kc[j] = *(const u32x4 *)(a.p.k + o);
-                    *(u32x4 *)vc[j] = *(const u32x4 *)(a.p.v + o);
-                } else {
-                    *(u32x2 *)kc[j] = *(const u32x2 *)(a.p.k + o);
-                    *(u32x2 *)vc[j] = *(const u32x2 *)(a.p.v + o);
-                }
-                ke[j] = a.p.ks[e];
-                ve[j] = a.p.vs[e];
+                c.k[j] = *(const words<CW> *)(a.p.k + o);
+                c.v[j] = *(const words<CW> *)(a.p.v + o);
+                c.ke[j] = a.p.ks[e];
+                c.ve[j] = a.p.vs[e];
             }
         };
-        const int last = s0 + n;
-        if (s0 + wave < last) {
-            find(s0 + wave);
-            fetch(s0 + wave);
-            find(min(s0 + wave + WAVES, last - 1));
-        }
-        for (int st = s0 + wave; st < last; st += WAVES) {
-            const int k0 = st * STEP;
-            const bool full = k0 + STEP <= min(ctx, kv_end);   // every row sees all of the step's keys
-            uint32_t seen[MT];                                 // otherwise: which of them the lane's row sees
-            if (!full) {
-                const int d = k0 - ctx, left = kv_end - k0;    // the same for all lanes
-                const uint32_t there = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1 : 0u;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-                    seen[mt] = there & (d >= 64 ? 0u : d >= 0 ? (uint32_t)(mask[mt] >> d) : d > -32 ? (uint32_t)mask[mt] << -d | ((1u << -d) - 1) : ~0u);
-            }
-            // ---- S^T = K Q^T
-            f32x4 sc[2][MT];
+        // S^T = K Q^T
+        auto scores = [&](const Codes<CW> &c, f32x4 (*sc)[MT]) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) sc[j][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-                const float s = ke[j] == NAN_EXP ? __builtin_nanf("") : exp_scale(ke[j]);
+                const float s = block_scale(c.ke[j]);
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    const bf16x8 kf = decode8(kc[j][ks], s);
+                    const bf16x8 kf = decode8(c.k[j][ks], s);
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                        for (int z = 0; z < NQ; ++z) sc[j][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][ks][z], sc[j][mt], 0, 0, 0);
+                        for (int z = 0; z < NQ; ++z) {
+                            const bf16x8 q = QLDS ? __builtin_bit_cast(bf16x8, qs[(mt * KS + ks) * 64 + l]) : qf[QLDS ? 0 : mt][ks][z];
+                            sc[j][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q, sc[j][mt], 0, 0, 0);
+                        }
                 }
             }
-            // ---- values to LDS, as rows
-            bool half_v = false;   // as fp16, and probabilities too
-            if (!F32) half_v = __builtin_amdgcn_ballot_w64(((ve[0] - HALF_LO) > HALF_HI - HALF_LO) | ((ve[1] - HALF_LO) > HALF_HI - HALF_LO)) == 0;
+        };
+        // With M the largest score so far times `scale`, a weight is 2^(score * scale - M), one multiply-add and one power; for fp16
+        // it is 2^8 of that, so that weights down to 2^-22 of the largest have all their bits.
+        auto weights = [&](int mt, float *p) {
+            float top = p[0], sum = 0.f;
+#pragma unroll
+            for (int e = 1; e < 8; ++e) top = fmaxf(top, p[e]);
+            const float m_new = fmaxf(m_run[mt], lane_groups_max(top) * a.scale);
+            const float m_use = m_new == -INFINITY ? 0.f : m_new;   // nothing seen so far: 2^(-inf), not 2^(-inf + inf)
+            const float alpha = __builtin_amdgcn_exp2f(m_run[mt] - m_use);
+            const float shift = (F32 ? 0.f : 8.f) - m_use;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], a.scale, shift));
+                sum += p[e];
+            }
+            m_run[mt] = m_new;
+            l_run[mt] = l_run[mt] * alpha + sum;
+            if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) acc[mt][dt] *= alpha;
+            }
+        };
+        // O^T += V^T P^T; slot (lane group g, element e) of the contraction is key 16 (e / 4) + 4 g + e % 4, which is where the scores
+        // lie.  Transposing load: lane i of 16 points at key row 4 g + i / 4, columns 16 dt + 4 (i % 4) .. and gets keys 4 g .. 4 g + 3
+        // of column 16 dt + i.
+        unsigned char *const put = vt + li * VS + lg * (DH / 2);
+        const unsigned char *const get = vt + (4 * lg + (li >> 2)) * VS + (li & 3) * 8;
+        auto values = [&](int dt) {
+            const bf16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(get + dt * 32));
+            const bf16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(get + dt * 32 + 16 * VS));
+            return __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        auto exact_product = [&](int mt, const float *p) {   // V in bfloat16, P in three pieces
+            bf16x8 pf[3];
+            split8<3>(p, pf);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const bf16x8 va = values(dt);
+#pragma unroll
+                for (int z = 0; z < 3; ++z) acc[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[z], acc[mt][dt], 0, 0, 0);
+            }
+        };
+        // A step of any kind: the ones at a sequence's end, and all of them where values leave fp16's range
+        auto any_step = [&](const Codes<CW> &c, int st) {
+            const int k0 = st * STEP, d = k0 - ctx, left = kv_end - k0;   // the same for all lanes
+            const uint32_t there = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1 : 0u;
+            uint32_t seen[MT];   // which keys the lane's row sees
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+                seen[mt] = there & (d >= 64 ? 0u : d >= 0 ? (uint32_t)(mask[mt] >> d) : d > -32 ? (uint32_t)mask[mt] << -d | ((1u << -d) - 1) : ~0u);
+            f32x4 sc[2][MT];
+            scores(c, sc);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float s = ve[j] == NAN_EXP ? __builtin_nanf("") : exp_scale(ve[j]);
-                uint32_t c[CW];
+                // A slot past the end counts for nothing whatever it holds.  A value that is not a number is kept from the rows that
+                // do not see it (0 times it would be one too): it is left out of the product, and the rows that do see it are marked.
+                const bool in = k0 + 16 * j + li < kv_end, nan = c.ve[j] == NAN_EXP, drop = !in | nan;
+                uint64_t bad = __builtin_amdgcn_ballot_w64(in & nan);
+                while (bad != 0) {
+                    const int at_lane = __builtin_ctzll(bad);
+                    bad &= bad - 1;
 #pragma unroll
-                for (int i = 0; i < CW; ++i) c[i] = vc[j][i];
-                if (!full) {
-                    // A slot past the end counts for nothing whatever it holds.  A value that is not a number is kept from the
-                    // rows that do not see it (0 times it would be one too): it is left out of the product here, and the rows
-                    // that do see it are marked.
-                    const bool in = k0 + 16 * j + li < kv_end;
-                    uint64_t bad = __builtin_amdgcn_ballot_w64(in & (ve[j] == NAN_EXP));
-                    while (bad != 0) {
-                        const int at_lane = __builtin_ctzll(bad);
-                        bad &= bad - 1;
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) nan_v[mt] |= ((seen[mt] >> (16 * j + (at_lane & 15))) & 1u) << (at_lane >> 4);
-                    }
-                    const bool drop = !in | (ve[j] == NAN_EXP);
-                    s = drop ? 1.f : s;
-#pragma unroll
-                    for (int i = 0; i < CW; ++i) c[i] = drop ? 0u : c[i];
+                    for (int mt = 0; mt < MT; ++mt) nan_v[mt] |= ((seen[mt] >> (16 * j + (at_lane & 15))) & 1u) << (at_lane >> 4);
                 }
-                unsigned char *to = vt + (16 * j + li) * VS + lg * (DH / 2);
-                if (half_v) {
+                const float s = drop ? 1.f : exp_scale(c.ve[j]);
 #pragma unroll
-                    for (int i = 0; i < CW; ++i) *(u32x4_alias *)(to + 16 * i) = __builtin_bit_cast(u32x4, decode8h(c[i], s));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < CW; ++i) *(u32x4_alias *)(to + 16 * i) = __builtin_bit_cast(u32x4, decode8(c[i], s));
-                }
+                for (int i = 0; i < CW; ++i) *(u32x4_alias *)(put + 16 * j * VS + 16 * i) = __builtin_bit_cast(u32x4, decode8(drop ? 0u : c.v[j][i], s));
             }
-            if (st + WAVES < last) {
-                fetch(st + WAVES);
-                find(min(st + 2 * WAVES, last - 1));
-            }
-            // ---- mask, softmax in powers of two
-            // With M the largest score so far times `scale`, a weight is 2^(score * scale - M), one multiply-add and one power; for
-            // fp16 it is 2^8 of that, so that weights down to 2^-22 of the largest have all their bits.
-            float p[MT][8];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
+                float p[8];
+                const uint32_t mine = seen[mt] >> (4 * lg);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[mt][e] = sc[e >> 2][mt][e & 3];
-                if (!full) {   // selects, not branches: lanes differ
-                    const uint32_t mine = seen[mt] >> (4 * lg);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) p[mt][e] = (mine >> (16 * (e >> 2) + (e & 3))) & 1u ? p[mt][e] : -INFINITY;
-                }
-                float top = p[mt][0], sum = 0.f;
-#pragma unroll
-                for (int e = 1; e < 8; ++e) top = fmaxf(top, p[mt][e]);
-                const float m_new = fmaxf(m_run[mt], lane_groups_max(top) * a.scale);
-                // nothing seen so far: the weights below are 2^(-inf), not 2^(-inf + inf)
-                const float m_use = (m_new == -INFINITY ? 0.f : m_new) - (F32 ? 0.f : 8.f);
-                const float alpha = __builtin_amdgcn_exp2f(m_run[mt] - (m_new == -INFINITY ? 0.f : m_new));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    p[mt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[mt][e], a.scale, -m_use));
-                    sum += p[mt][e];
-                }
-                m_run[mt] = m_new;
-                l_run[mt] = l_run[mt] * alpha + sum;
-                if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) acc[mt][dt] *= alpha;
-                }
+                for (int e = 0; e < 8; ++e) p[e] = (mine >> (16 * (e >> 2) + (e & 3))) & 1u ? sc[e >> 2][mt][e & 3] : -INFINITY;
+                weights(mt, p);
+                exact_product(mt, p);
             }
-            // ---- O^T += V^T P^T; slot (lane group g, element e) of the contraction is key 16 (e / 4) + 4 g + e % 4, which is
-            // where the scores lie.  Transposing load: lane i of 16 points at key row 4 g + i / 4, columns 16 dt + 4 (i % 4) ..
-            // and gets keys 4 g .. 4 g + 3 of column 16 dt + i.
-            const unsigned char *from = vt + (4 * lg + (li >> 2)) * VS + (li & 3) * 8;
-            auto values = [&](int dt) {
-                const bf16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(from + dt * 32));
-                const bf16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(from + dt * 32 + 16 * VS));
-                return __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7);
-            };
-            if (half_v) {
-                f16x8 ph[MT];
+        };
+        // A step whose keys every row sees; V and P in fp16 where the output is bfloat16
+        unsigned beyond = 0;   // whether a value was outside fp16's range: then it is all done again
+        auto full_step = [&](const Codes<CW> &c) {
+            f32x4 sc[2][MT];
+            scores(c, sc);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-                    ph[mt] = __builtin_convertvector((f32x8){p[mt][0], p[mt][1], p[mt][2], p[mt][3], p[mt][4], p[mt][5], p[mt][6], p[mt][7]}, f16x8);
+            for (int j = 0; j < 2; ++j) {
+                const float s = block_scale(c.ve[j]);
+                if (!F32) beyond |= c.ve[j] - HALF_LO > HALF_HI - HALF_LO;
+#pragma unroll
+                for (int i = 0; i < CW; ++i)
+                    *(u32x4_alias *)(put + 16 * j * VS + 16 * i) =
+                        F32 ? __builtin_bit_cast(u32x4, decode8(c.v[j][i], s)) : __builtin_bit_cast(u32x4, decode8h(c.v[j][i], s));
+            }
+            f16x8 ph[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                float p[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = sc[e >> 2][mt][e & 3];
+                weights(mt, p);
+                if (F32) exact_product(mt, p);
+                else ph[mt] = __builtin_convertvector((f32x8){p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]}, f16x8);
+            }
+            if (!F32)
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
                     const f16x8 va = __builtin_bit_cast(f16x8, values(dt));
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) acc[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ph[mt], acc[mt][dt], 0, 0, 0);
                 }
-            } else {
+        };
+        // ---- The wave's steps, its last one first: of the steps in which rows differ (at most three, at the sequence's end) a wave
+        // has one at most, and its codes come with those of the first others.  Of these, codes are asked for AHEAD steps ahead and page
+        // numbers one more; what is under way is the same at every turn, so that a wait is for the step at hand alone.
+        const int st = s0 + wave, mine = (last - st + NW - 1) / NW;
+        const int open = min(mine, max(0, (min(ctx, kv_end) / STEP - st + NW - 1) / NW));   // those that every row sees
+        if (mine > 0) {
+            int page[AHEAD + 1][2], page_end[2];
+            Codes<CW> c[AHEAD], c_end;
+            find(page_end, st + (mine - 1) * NW);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {   // tile by tile: the rare case needs few registers (one tile where it is the only one)
-                    bf16x8 pf[3];
-                    split8<3>(p[mt], pf);
+            for (int u = 0; u <= AHEAD; ++u) find(page[u], st + u * NW);
+            fetch(c_end, page_end, st + (mine - 1) * NW);
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        const bf16x8 va = values(dt);
+            for (int u = 0; u < AHEAD; ++u) fetch(c[u], page[u], st + u * NW);
+            if (open < mine) any_step(c_end, st + (mine - 1) * NW);
+            for (int i = 0; i < open; i += AHEAD)
 #pragma unroll
-                        for (int z = 0; z < 3; ++z) acc[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[z], acc[mt][dt], 0, 0, 0);
-                    }
+                for (int u = 0; u < AHEAD; ++u) {
+                    if (i + u < open) full_step(c[u]);
+                    fetch(c[u], page[AHEAD], st + (i + u + AHEAD) * NW);
+                    find(page[AHEAD], st + (i + u + AHEAD + 1) * NW);
                 }
+            // values outside fp16's range, or more than one step to be masked (a cut-off sequence): step by step
+            const bool again = !F32 && __builtin_amdgcn_ballot_w64(beyond) != 0;
+            if (again) reset();
+            for (int i = again ? 0 : open; i < (again ? mine : mine - 1); ++i) {
+                find(page_end, st + i * NW);
+                fetch(c_end, page_end, st + i * NW);
+                any_step(c_end, st + i * NW);
             }
         }
         // ---- the waves meet, one row tile at a time; wave w then has DT / 4 of its 16-dimension pieces
         const int which = at == begin ? 0 : 1;
-        const bool whole = n == nsteps;
-        f32x4_alias *mo = (f32x4_alias *)vt_all;   // [WAVES][DT][64]
+        const bool whole = WHOLE || n == nsteps;
+        f32x4_alias *mo = (f32x4_alias *)vt_all;   // [NW][DT][64]
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             if (__builtin_amdgcn_ballot_w64(nan_v[mt] != 0) != 0) {
@@ -636,22 +690,23 @@ __global__ __launch_bounds__(NT, 2) void k_paged_attend(AttendArgs a) {
                 mm[wave][li][1] = lsum;
             }
             __syncthreads();
-            float M = -INFINITY, L = 0.f, f[WAVES];
+            float M = -INFINITY, L = 0.f, f[NW];
 #pragma unroll
-            for (int v = 0; v < WAVES; ++v) M = fmaxf(M, mm[v][li][0]);
+            for (int v = 0; v < NW; ++v) M = fmaxf(M, mm[v][li][0]);
             const float m_use = M == -INFINITY ? 0.f : M;
 #pragma unroll
-            for (int v = 0; v < WAVES; ++v) {
+            for (int v = 0; v < NW; ++v) {
                 f[v] = __builtin_amdgcn_exp2f(mm[v][li][0] - m_use);
                 L += f[v] * mm[v][li][1];
             }
             const int r = row0 + mt * 16 + li, t = r / G, g = r - t * G;
 #pragma unroll
-            for (int i = 0; i < DT / WAVES; ++i) {
-                const int dt = wave * (DT / WAVES) + i;
+            for (int i = 0; i < (DT + NW - 1) / NW; ++i) {
+                const int dt = wave * ((DT + NW - 1) / NW) + i;
+                if (DT < NW && dt >= DT) continue;
                 f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int v = 0; v < WAVES; ++v) o += f[v] * (f32x4)mo[(v * DT + dt) * 64 + l];
+                for (int v = 0; v < NW; ++v) o += f[v] * (f32x4)mo[(v * DT + dt) * 64 + l];
                 if (t >= a.rows) continue;
                 if (whole) {
                     o *= L == 0.f ? 0.f : 1.f / L;   // a row that sees nothing is zero
@@ -669,7 +724,7 @@ __global__ __launch_bounds__(NT, 2) void k_paged_attend(AttendArgs a) {
             }
         }
         __syncthreads();
-        at += n;
+        at += part;
     }
 }
 
@@ -684,8 +739,8 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
     const int item_ = blockIdx.x / MT, mt = blockIdx.x % MT, b = item_ / items, item = item_ - b * items;
     const int nsteps = steps_of(end_of(a, b)), lane = b / sh.per;
     int base = __builtin_amdgcn_readlane(sh.before, lane);
-    for (int i = lane * sh.per; i < b; ++i) base += items * steps_of(end_of(a, i));
-    const int from = base + item * nsteps, to = from + nsteps;
+    for (int i = lane * sh.per; i < b; ++i) base += items * (steps_of(end_of(a, i)) + PER_ITEM);
+    const int from = base + item * (nsteps + PER_ITEM), to = from + nsteps;
     const int w0 = sh.owner(from), w1 = sh.owner(to - 1);
     if (w0 == w1) return;   // one workgroup had all of it
     const int G = a.n_heads / a.p.n_kv, h = item / a.groups;
@@ -695,18 +750,34 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
     float M = -INFINITY, L = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int w = w0; w <= w1; ++w) {
-        const size_t pr = ((size_t)w * 2 + (sh.first(w) >= from ? 0 : 1)) * (MT * 16) + mt * 16 + li;
-        const float m = a.ml[pr * 2], ls = a.ml[pr * 2 + 1];
-        const float m_new = fmaxf(M, m), m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float fo = __builtin_amdgcn_exp2f(M - m_use), fn = __builtin_amdgcn_exp2f(m - m_use);
+    constexpr int PARTS = 4;   // requested at once
+    for (int w = w0; w <= w1; w += PARTS) {
+        float m[PARTS], ls[PARTS];
+        f32x4 x[PARTS][E / 4];
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            const int v = min(w + i, w1);
+            const size_t pr = ((size_t)v * 2 + (sh.first(v) >= from ? 0 : 1)) * (MT * 16) + mt * 16 + li;
+            m[i] = w + i <= w1 ? a.ml[pr * 2] : -INFINITY;
+            ls[i] = a.ml[pr * 2 + 1];
+#pragma unroll
+            for (int e = 0; e < E / 4; ++e) x[i][e] = *(const f32x4 *)(a.part + pr * DH + d0 + 4 * e);
+        }
+        float m_new = M;
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) m_new = fmaxf(m_new, m[i]);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new, fo = __builtin_amdgcn_exp2f(M - m_use);
         M = m_new;
-        L = L * fo + ls * fn;
+        L *= fo;
 #pragma unroll
-        for (int e = 0; e < E; e += 4) {
-            const f32x4 x = *(const f32x4 *)(a.part + pr * DH + d0 + e);
+        for (int e = 0; e < E; ++e) o[e] *= fo;
 #pragma unroll
-            for (int z = 0; z < 4; ++z) o[e + z] = o[e + z] * fo + x[z] * fn;
+        for (int i = 0; i < PARTS; ++i) {
+            if (w + i > w1) continue;   // the same for all lanes; a part of none but not-a-number would count otherwise
+            const float f = __builtin_amdgcn_exp2f(m[i] - m_use);
+            L += ls[i] * f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] += x[i][e >> 2][e & 3] * f;
         }
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
@@ -769,12 +840,20 @@ int compute_units() {
     }();
     return n;
 }
-enum { ATTEND_WGS_MAX = 1024 };   // what the workspace is sized for
+enum { ATTEND_WGS_MAX = 512 };   // what the workspace is sized for
+
+// Whether every item is left to one workgroup, which spares the second launch.  (us)
+bool attend_whole(int items, int steps, int cu) { return items <= cu ? steps <= 80 : steps <= 16; }
 
 template <int DH, int MT, bool F32>
-void launch_attend(hipStream_t st, const AttendArgs &a) {
-    k_paged_attend<DH, MT, F32><<<a.wgs, NT, 0, st>>>(a);
-    k_paged_join<DH, MT, F32><<<(unsigned)a.batch * a.p.n_kv * a.groups * MT, 256, 0, st>>>(a);
+void launch_attend(hipStream_t st, const AttendArgs &a, int cu) {
+    const int items = a.batch * a.p.n_kv * a.groups;
+    if (attend_whole(items, a.max_len / STEP, cu)) {
+        k_paged_attend<DH, MT, F32, true><<<items, 512, 0, st>>>(a);
+    } else {
+        k_paged_attend<DH, MT, F32, false><<<a.wgs, 64 * WAVES, 0, st>>>(a);
+        k_paged_join<DH, MT, F32><<<items * MT, 256, 0, st>>>(a);
+    }
 }
 
 }  // namespace
@@ -894,19 +973,20 @@ koala_status koala_paged_attend(const koala_paged_kv *kv, void *hip_stream, int 
     a.scale = scale * LOG2E;
     const int room = kv->pages_per_seq * kv->page_size;
     a.max_len = max_len > 0 && max_len < room ? max_len : room;
-    if ((double)batch * KV * a.groups * (a.max_len / STEP + 1) > 2147483647.0) return KOALA_E_SHAPE;   // steps are counted in 32 bits
-    a.wgs = attend_wgs(compute_units());
+    if ((double)batch * KV * a.groups * (a.max_len / STEP + 1 + PER_ITEM) > 2147483647.0) return KOALA_E_SHAPE;   // steps are counted in 32 bits
+    const int cu = compute_units();
+    a.wgs = attend_wgs(cu);
     if (a.wgs > ATTEND_WGS_MAX) a.wgs = ATTEND_WGS_MAX;
     a.q = q; a.ldq = (size_t)q_stride; a.out = out;
     a.part = (float *)workspace;
     a.ml = a.part + (size_t)a.wgs * 2 * MT * 16 * DH;
     hipStream_t st = (hipStream_t)hip_stream;
     if (DH == 128) {
-        if (dtype == KOALA_FP32) launch_attend<128, 1, true>(st, a);
-        else MT == 1 ? launch_attend<128, 1, false>(st, a) : launch_attend<128, 2, false>(st, a);
+        if (dtype == KOALA_FP32) launch_attend<128, 1, true>(st, a, cu);
+        else MT == 1 ? launch_attend<128, 1, false>(st, a, cu) : launch_attend<128, 2, false>(st, a, cu);
     } else {
-        if (dtype == KOALA_FP32) launch_attend<64, 1, true>(st, a);
-        else MT == 1 ? launch_attend<64, 1, false>(st, a) : launch_attend<64, 2, false>(st, a);
+        if (dtype == KOALA_FP32) launch_attend<64, 1, true>(st, a, cu);
+        else MT == 1 ? launch_attend<64, 1, false>(st, a, cu) : launch_attend<64, 2, false>(st, a, cu);
     }
     return launched();
 }
