@@ -84,11 +84,12 @@ def library_path() -> str:
 
 
 _LIB = None
+torch = None     # imported with the library
 
 
 def load_library():
     """Load libkoala.so; there is no fallback - a missing library is an error."""
-    global _LIB
+    global _LIB, torch
     if _LIB is not None:
         return _LIB
     path = library_path()
@@ -97,7 +98,7 @@ def load_library():
                              "(or __graft_entry__.build())")
     # PyTorch first: it ships its own HIP runtime, and the pointers and streams handed to the library come
     # from it.  Loading the library before torch would bring a second runtime into the process.
-    import torch  # noqa: F401
+    import torch
     lib = C.CDLL(path)
     vp, ip = C.c_void_p, C.c_int
     lib.koala_create.argtypes = [C.POINTER(_Shape), C.POINTER(_DraftShape), C.POINTER(_Tree), ip, C.POINTER(vp)]
@@ -394,56 +395,72 @@ class MedusaHeadTrainer:
 
 # ---------------------------------------------------------------------------------------------------------------
 # 8-bit projections and the 4-bit paged cache.  A tensor's type, place and layout are known here only, so they are
-# checked here; sizes, strides and alignment are checked by the library.
+# checked here; sizes, strides and alignment are checked by the library.  Small calls are as long as their way through
+# Python, so each check asks a tensor as little as it can.
 # ---------------------------------------------------------------------------------------------------------------
 def _refuse(name, msg):
     raise KoalaError(STATUS_BY_NAME[name], msg)
 
 
-def _dtype(t, what):
-    import torch
-    if t.dtype == torch.bfloat16:
-        return KOALA_BF16
-    if t.dtype != torch.float32:
-        _refuse("KOALA_E_UNSUPPORTED", f"{what}: bfloat16 or float32 wanted, got {t.dtype}")
-    return KOALA_FP32
+_TYPES = {}      # torch types by their KOALA numbers, filled with the library's first use
+
+
+def _float_type(t, what):
+    if not _TYPES:
+        _TYPES.update({torch.float32: KOALA_FP32, torch.bfloat16: KOALA_BF16})
+    n = _TYPES.get(t.dtype)
+    if n is None or not t.is_cuda:
+        _refuse("KOALA_E_UNSUPPORTED", f"{what}: bfloat16 or float32 on the device wanted, got {t.dtype} on {t.device}")
+    return n
 
 
 def _of(t, dtype, what, shape=None):
     """The address of a dense device tensor of the given type and shape."""
     if t.dtype != dtype or not t.is_cuda:
         _refuse("KOALA_E_UNSUPPORTED", f"{what}: {dtype} on the device wanted, got {t.dtype} on {t.device}")
-    if not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+    if (shape is not None and t.shape != shape) or not t.is_contiguous():
         _refuse("KOALA_E_SHAPE", f"{what}: dense {shape if shape is not None else ''} wanted, got {tuple(t.shape)} strides {t.stride()}")
     return t.data_ptr()
 
 
-def _matrix(t, what):
-    """Address and row stride of a device matrix whose rows are dense."""
-    if not t.is_cuda:
-        _refuse("KOALA_E_UNSUPPORTED", f"{what}: a device tensor wanted")
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+def _row_stride(t, rows, cols, what):
+    """Row stride of a matrix [rows, cols] whose rows are dense."""
+    try:
+        r, c = t.stride()
+    except ValueError:
+        r, c = 0, 0
+    if (c != 1 and cols > 1) or t.dim() != 2:
         _refuse("KOALA_E_SHAPE", f"{what}: a matrix of dense rows wanted, got {tuple(t.shape)} strides {t.stride()}")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+    return r if rows > 1 else max(r, cols)
 
 
 def _heads(t, batch, rows, head_dim, what):
-    """Number of heads and row stride of a device tensor [batch, rows, heads, head_dim] whose rows are dense and evenly spaced."""
-    if not t.is_cuda:
-        _refuse("KOALA_E_UNSUPPORTED", f"{what}: a device tensor wanted")
-    sb, sr, sh, sd = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
-    if t.dim() != 4 or t.shape[0] != batch or t.shape[1] != rows or t.shape[3] != head_dim or sd != 1 or (t.shape[2] > 1 and sh != head_dim):
+    """Number of heads and row stride of a tensor [batch, rows, heads, head_dim] whose rows are dense and evenly spaced."""
+    try:
+        b, r, heads, d = t.shape
+        sb, sr, sh, sd = t.stride()
+    except ValueError:
+        b = None
+    if b != batch or r != rows or d != head_dim or sd != 1 or (sh != head_dim and heads > 1):
         _refuse("KOALA_E_SHAPE", f"{what}: [{batch}, {rows}, heads, {head_dim}] of dense rows wanted, got {tuple(t.shape)} strides {t.stride()}")
-    if rows > 1:
-        if batch > 1 and sb != rows * sr:
-            _refuse("KOALA_E_SHAPE", f"{what}: rows are not evenly spaced (strides {t.stride()})")
-        return t.shape[2], sr
-    return t.shape[2], (sb if batch > 1 else t.shape[2] * head_dim)
+    if rows == 1:
+        return heads, (sb if batch > 1 else heads * head_dim)
+    if sb != rows * sr and batch > 1:
+        _refuse("KOALA_E_SHAPE", f"{what}: rows are not evenly spaced (strides {t.stride()})")
+    return heads, sr
 
 
-def _raw_stream(stream):
-    import torch
-    return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+def _stream_of(t, stream):
+    """The raw stream to enqueue on: the one given, or the current one of the tensor's device."""
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(t.get_device())
+
+
+def _raw_stream(device):
+    global _raw_stream
+    _raw_stream = torch._C._cuda_getCurrentRawStream     # the handle alone: torch.cuda.current_stream() takes 3 us to wrap it
+    return _raw_stream(device)
 
 
 class _Workspaces:
@@ -455,36 +472,37 @@ class _Workspaces:
     def get(self, raw, need, device, stream):
         ws = self._by_stream.get(raw)
         if ws is None or ws.numel() < need:
-            import torch
             with torch.cuda.stream(stream):
                 ws = self._by_stream[raw] = torch.empty(need, dtype=torch.uint8, device=device)
-        return ws
+        return ws.data_ptr()
 
 
 def quantize_rows(x, q, scale, form="plain", gain=None, eps=1e-6, stream=None):
     """Rows of x (bfloat16 or float32) to int8 rows q with a scale each (koala_quantize_rows).  form "norm": RMSNorm with `gain` first;
     "swiglu": SiLU(gate) * up of x's interleaved pairs.  q may be wider than the row: bytes up to the next 16 are zeroed."""
-    import torch
-    if form not in _ROW_FORMS:
+    lib = load_library()
+    kind = _ROW_FORMS.get(form)
+    if kind is None:
         _refuse("KOALA_E_UNSUPPORTED", f"form {form!r}")
-    xt = _dtype(x, "x")
-    xp, xs = _matrix(x, "x")
-    qp, qs = _matrix(q, "q")
-    rows, cols = x.shape
-    if form == "swiglu":
-        if cols % 2:
+    xt = _float_type(x, "x")
+    rows, width = x.shape
+    xs = _row_stride(x, rows, width, "x")
+    cols = width
+    if kind == KOALA_ROWS_SWIGLU:
+        cols = width // 2
+        if cols * 2 != width:
             _refuse("KOALA_E_SHAPE", "x: pairs of gate and up wanted")
-        cols //= 2
-    if q.dtype != torch.int8:
-        _refuse("KOALA_E_UNSUPPORTED", f"q: int8 wanted, got {q.dtype}")
-    if q.shape[0] != rows or q.shape[1] < cols:
+    if q.dtype != torch.int8 or not q.is_cuda:
+        _refuse("KOALA_E_UNSUPPORTED", f"q: int8 on the device wanted, got {q.dtype} on {q.device}")
+    q_rows, q_cols = q.shape
+    if q_rows != rows or q_cols < cols:
         _refuse("KOALA_E_SHAPE", f"q: [{rows}, {cols}] wanted, got {tuple(q.shape)}")
     gp, gt = 0, 0
-    if form == "norm" and gain is not None:
-        gt = _dtype(gain, "gain")
+    if kind == KOALA_ROWS_NORM and gain is not None:
+        gt = _float_type(gain, "gain")
         gp = _of(gain, gain.dtype, "gain", (cols,))
-    rc = load_library().koala_quantize_rows(_raw_stream(stream), _ROW_FORMS[form], xt, rows, cols, xp, xs, gp, gt, eps, qp, qs,
-                                            _of(scale, torch.float32, "scale", (rows,)))
+    rc = lib.koala_quantize_rows(_stream_of(x, stream), kind, xt, rows, cols, x.data_ptr(), xs, gp, gt, eps, q.data_ptr(),
+                                            _row_stride(q, rows, q_cols, "q"), _of(scale, torch.float32, "scale", (rows,)))
     if rc != 0:
         raise KoalaError(rc, "koala_quantize_rows")
 
@@ -493,13 +511,12 @@ class QuantizedLinear:
     """A Linear weight in 8 bits: w int8 [out_features, in_features] (rows may be strided) and w_scale fp32 [out_features], borrowed."""
 
     def __init__(self, w, w_scale):
-        import torch
         self.lib = load_library()
-        if w.dtype != torch.int8:
-            _refuse("KOALA_E_UNSUPPORTED", f"w: int8 wanted, got {w.dtype}")
+        if w.dtype != torch.int8 or not w.is_cuda:
+            _refuse("KOALA_E_UNSUPPORTED", f"w: int8 on the device wanted, got {w.dtype} on {w.device}")
         self.w, self.w_scale = w, w_scale
         self.out_features, self.in_features = w.shape
-        self._wp, self._ws = _matrix(w, "w")
+        self._wp, self._ws = w.data_ptr(), _row_stride(w, *w.shape, "w")
         self._sp = _of(w_scale, torch.float32, "w_scale", (self.out_features,))
         self._need, self._workspaces = {}, _Workspaces()
 
@@ -514,30 +531,26 @@ class QuantizedLinear:
     def forward(self, q, scale, y, add=None, stream=None):
         """y = scale * w_scale * (q w^T) (+ add, which may be y): q int8 [rows, >= in_features] and scale from quantize_rows, y
         bfloat16 or float32 [rows, out_features]."""
-        import torch
-        rows = q.shape[0]
-        if q.dtype != torch.int8:
-            _refuse("KOALA_E_UNSUPPORTED", f"q: int8 wanted, got {q.dtype}")
-        qp, qs = _matrix(q, "q")
-        yt = _dtype(y, "y")
-        yp, ys = _matrix(y, "y")
-        if q.shape[1] < self.in_features or tuple(y.shape) != (rows, self.out_features):
+        if q.dtype != torch.int8 or not q.is_cuda:
+            _refuse("KOALA_E_UNSUPPORTED", f"q: int8 on the device wanted, got {q.dtype} on {q.device}")
+        rows, cols = q.shape
+        out = self.out_features
+        yt = _float_type(y, "y")
+        if cols < self.in_features or y.shape != (rows, out):
             _refuse("KOALA_E_SHAPE", f"q {tuple(q.shape)}, y {tuple(y.shape)} for a weight {tuple(self.w.shape)}")
+        ys = _row_stride(y, rows, out, "y")
         ap = 0
         if add is not None:
-            ap, a_stride = _matrix(add, "add")
-            if add.dtype != y.dtype or add.shape != y.shape or (rows > 1 and a_stride != ys):
-                _refuse("KOALA_E_SHAPE", "add: the type, shape and strides of y wanted")
+            if add.dtype != y.dtype or add.shape != y.shape or not add.is_cuda or _row_stride(add, rows, out, "add") != ys:
+                _refuse("KOALA_E_SHAPE", "add: the type, shape, strides and device of y wanted")
+            ap = add.data_ptr()
         need = self._need.get(rows)
         if need is None:
             need = self._workspace_bytes(rows)
-        wp = 0
-        raw = _raw_stream(stream)
-        if need:
-            wp = self._workspaces.get(raw, need, y.device, stream).data_ptr()
-        rc = self.lib.koala_linear_quantized(raw, rows, self.out_features, self.in_features, qp, qs,
-                                             _of(scale, torch.float32, "scale", (rows,)), self._wp, self._ws, self._sp, yt, ap, yp, ys,
-                                             wp, need)
+        raw = _stream_of(q, stream)
+        rc = self.lib.koala_linear_quantized(raw, rows, out, self.in_features, q.data_ptr(), _row_stride(q, rows, cols, "q"),
+                                             _of(scale, torch.float32, "scale", (rows,)), self._wp, self._ws, self._sp, yt, ap,
+                                             y.data_ptr(), ys, self._workspaces.get(raw, need, y.device, stream) if need else 0, need)
         if rc != 0:
             raise KoalaError(rc, "koala_linear_quantized")
 
@@ -548,7 +561,6 @@ class PagedCache:
     int32 [max_batch].  `alloc_paged_cache` makes the pools."""
 
     def __init__(self, k, v, k_scale, v_scale, page_table, ctx_len):
-        import torch
         self.lib = load_library()
         if k.dim() != 5 or page_table.dim() != 2:
             _refuse("KOALA_E_SHAPE", "k: five dimensions wanted; page_table: two")
@@ -565,6 +577,7 @@ class PagedCache:
         need = C.c_size_t()
         self._check(self.lib.koala_paged_workspace_bytes(self._ref, C.byref(need)), "koala_paged_workspace_bytes")
         self._need, self._workspaces = need.value, _Workspaces()
+        self._scale = self.head_dim ** -0.5
 
     @staticmethod
     def _check(rc, name):
@@ -574,68 +587,74 @@ class PagedCache:
     def append(self, layer, q, k, v, q_out, rope_cos, rope_sin, depth=None, n_new=None, stream=None):
         """Rotate and append the new rows of every sequence: q [batch, rows, heads, head_dim] (may be None), k, v [batch, rows,
         kv_heads, head_dim], possibly parts of one array; q_out dense.  See koala_paged_append."""
-        import torch
-        batch, rows = k.shape[0], k.shape[1]
-        dt = _dtype(k, "k")
-        hk, ldk = _heads(k, batch, rows, self.head_dim, "k")
-        hv, ldv = _heads(v, batch, rows, self.head_dim, "v")
-        if hk != self.n_kv_heads or hv != hk or v.dtype != k.dtype:
-            _refuse("KOALA_E_SHAPE", f"k, v: {self.n_kv_heads} heads of one type wanted")
+        dt = _float_type(k, "k")
+        if k.dim() != 4:
+            _refuse("KOALA_E_SHAPE", f"k: [batch, rows, kv_heads, head_dim] wanted, got {tuple(k.shape)}")
+        batch, rows, dh = k.shape[0], k.shape[1], self.head_dim
+        hk, ldk = _heads(k, batch, rows, dh, "k")
+        hv, ldv = _heads(v, batch, rows, dh, "v")
+        if hk != self.n_kv_heads or hv != hk or v.dtype != k.dtype or not v.is_cuda:
+            _refuse("KOALA_E_SHAPE", f"k, v: {self.n_kv_heads} heads of one type and device wanted")
         heads, ldq, qp, op = 0, 0, 0, 0
         if q is not None:
-            heads, ldq = _heads(q, batch, rows, self.head_dim, "q")
-            if q.dtype != k.dtype:
-                _refuse("KOALA_E_UNSUPPORTED", "q: the type of k wanted")
-            qp, op = q.data_ptr(), _of(q_out, k.dtype, "q_out", (batch, rows, heads, self.head_dim))
-        half = self.head_dim // 2
-        table = (rope_cos.shape[0], half)
-        self._check(self.lib.koala_paged_append(
-            self._ref, _raw_stream(stream), layer, batch, rows, dt, heads, qp, ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+            heads, ldq = _heads(q, batch, rows, dh, "q")
+            if q.dtype != k.dtype or not q.is_cuda:
+                _refuse("KOALA_E_UNSUPPORTED", "q: the type and device of k wanted")
+            qp, op = q.data_ptr(), _of(q_out, k.dtype, "q_out", (batch, rows, heads, dh))
+        table = (rope_cos.shape[0], dh // 2)
+        rc = self.lib.koala_paged_append(
+            self._ref, _stream_of(k, stream), layer, batch, rows, dt, heads, qp, ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
             0 if n_new is None else _of(n_new, torch.int32, "n_new", (batch,)),
             0 if depth is None else _of(depth, torch.int32, "depth", (rows,)), _of(rope_cos, torch.float32, "rope_cos", table),
-            _of(rope_sin, torch.float32, "rope_sin", table), table[0], op), "koala_paged_append")
+            _of(rope_sin, torch.float32, "rope_sin", table), table[0], op)
+        if rc != 0:
+            raise KoalaError(rc, "koala_paged_append")
 
     def read(self, layer, start, k_out, v_out, stream=None):
         """Slots start[b] .. (start None: from 0) of one layer (k_out, v_out [batch, n, kv_heads, head_dim]) or of all
         (layer None: [layers, batch, n, kv_heads, head_dim]) as the values they stand for, bfloat16 or float32."""
-        import torch
-        dt = _dtype(k_out, "k_out")
-        shape = tuple(k_out.shape)
-        if len(shape) != (5 if layer is None else 4) or shape[-2:] != (self.n_kv_heads, self.head_dim) or (layer is None and shape[0] != self.n_layers):
-            _refuse("KOALA_E_SHAPE", f"k_out: got {shape}")
+        dt = _float_type(k_out, "k_out")
+        shape = k_out.shape
+        if len(shape) != (5 if layer is None else 4) or shape[-1] != self.head_dim or shape[-2] != self.n_kv_heads or (
+                layer is None and shape[0] != self.n_layers):
+            _refuse("KOALA_E_SHAPE", f"k_out: got {tuple(shape)}")
         batch, n = shape[-4], shape[-3]
-        self._check(self.lib.koala_paged_read(
-            self._ref, _raw_stream(stream), layer or 0, self.n_layers if layer is None else 1, batch,
+        rc = self.lib.koala_paged_read(
+            self._ref, _stream_of(k_out, stream), layer or 0, self.n_layers if layer is None else 1, batch,
             0 if start is None else _of(start, torch.int32, "start", (batch,)), n, dt, _of(k_out, k_out.dtype, "k_out"),
-            _of(v_out, k_out.dtype, "v_out", shape)), "koala_paged_read")
+            _of(v_out, k_out.dtype, "v_out", shape))
+        if rc != 0:
+            raise KoalaError(rc, "koala_paged_read")
 
     def attend(self, layer, q, out, mask=None, scale=None, max_len=0, stream=None):
         """Attention of the new rows (already appended) over the cache: q [batch, rows <= 64, heads, head_dim] rotated, out dense.
         mask: int64 [rows] or [batch, rows], bit j of a row's set if it sees new row j (tree_masks); None: rows up to its own."""
-        import torch
-        if q.dim() != 4:
-            _refuse("KOALA_E_SHAPE", f"q: [batch, rows, heads, head_dim] wanted, got {tuple(q.shape)}")
-        batch, rows = q.shape[0], q.shape[1]
-        dt = _dtype(q, "q")
+        dt = _float_type(q, "q")
+        shape = q.shape
+        if len(shape) != 4:
+            _refuse("KOALA_E_SHAPE", f"q: [batch, rows, heads, head_dim] wanted, got {tuple(shape)}")
+        batch, rows = shape[0], shape[1]
         heads, ldq = _heads(q, batch, rows, self.head_dim, "q")
         mp, ms = 0, 0
         if mask is not None:
-            per_seq = mask.dim() == 2
-            mp, ms = _of(mask, torch.int64, "mask", (batch, rows) if per_seq else (rows,)), (rows if per_seq else 0)
-        raw = _raw_stream(stream)
-        ws = self._workspaces.get(raw, self._need, q.device, stream)
-        self._check(self.lib.koala_paged_attend(
-            self._ref, raw, layer, batch, rows, dt, heads, q.data_ptr(), ldq, mp, ms,
-            self.head_dim ** -0.5 if scale is None else scale, max_len,
-            _of(out, q.dtype, "out", (batch, rows, heads, self.head_dim)), ws.data_ptr(), self._need), "koala_paged_attend")
+            ms = rows if mask.dim() == 2 else 0
+            mp = _of(mask, torch.int64, "mask", (batch, rows) if ms else (rows,))
+        raw = _stream_of(q, stream)
+        rc = self.lib.koala_paged_attend(
+            self._ref, raw, layer, batch, rows, dt, heads, q.data_ptr(), ldq, mp, ms, self._scale if scale is None else scale, max_len,
+            _of(out, q.dtype, "out", shape), self._workspaces.get(raw, self._need, q.device, stream), self._need)
+        if rc != 0:
+            raise KoalaError(rc, "koala_paged_attend")
 
     def commit(self, accept_len, accept_path, new_len=None, stream=None):
         """Move the accepted paths' rows behind the context in every layer; new_len (default: ctx_len itself) becomes the new lengths."""
-        import torch
-        batch = accept_len.shape[0]
+        i32, batch = torch.int32, accept_len.shape[0]
         if accept_path.dim() != 2:
             _refuse("KOALA_E_SHAPE", "accept_path: [batch, depth + 1] wanted")
-        self._check(self.lib.koala_paged_commit(
-            self._ref, _raw_stream(stream), batch, _of(accept_len, torch.int32, "accept_len", (batch,)),
-            _of(accept_path, torch.int32, "accept_path", (batch, accept_path.shape[1])), accept_path.shape[1],
-            self._kv.ctx_len if new_len is None else _of(new_len, torch.int32, "new_len", (batch,))), "koala_paged_commit")
+        stride = accept_path.shape[1]
+        rc = self.lib.koala_paged_commit(
+            self._ref, _stream_of(accept_len, stream), batch, _of(accept_len, i32, "accept_len", (batch,)),
+            _of(accept_path, i32, "accept_path", (batch, stride)), stride,
+            self._kv.ctx_len if new_len is None else _of(new_len, i32, "new_len", (batch,)))
+        if rc != 0:
+            raise KoalaError(rc, "koala_paged_commit")

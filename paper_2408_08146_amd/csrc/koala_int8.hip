@@ -1,10 +1,7 @@
 // Projections in 8-bit integers with a scale for each token and each output channel (koala.h, "Projections in 8-bit integers").
 #include "koala_internal.h"
-#include <stdlib.h>
+#include <cmath>
 
-#ifndef KCS
-#define KCS 256
-#endif
 namespace {
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
@@ -66,6 +63,13 @@ __device__ __forceinline__ unsigned wave_max(unsigned x) {
     return x;
 }
 
+// e^x to about two units in the last place: a power of two, and what its argument's rounding left out
+__device__ __forceinline__ float exp_of(float x) {
+    const float t = x * 1.44269504f, left = __builtin_fmaf(x, 1.44269504f, -t) + x * 1.92596299e-8f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return t < 120.f ? __builtin_fmaf(e, left * 0.693147181f, e) : e;   // (beyond, an infinity is one)
+}
+
 template <int FORM, bool F32, int CH>
 __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
     __shared__ float s_sum[16];
@@ -82,7 +86,7 @@ __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
             load8<F32>(a.x, from, 16 * c, 2 * cols, p);
             load8<F32>(a.x, from, 16 * c + 8, 2 * cols, p + 8);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = p[2 * e] / (1.f + expf(-p[2 * e])) * p[2 * e + 1];
+            for (int e = 0; e < 8; ++e) x[e] = p[2 * e] * __builtin_amdgcn_rcpf(1.f + exp_of(-p[2 * e])) * p[2 * e + 1];
         } else {
             load8<F32>(a.x, from, 8 * c, cols, x);
         }
@@ -157,11 +161,18 @@ __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
     float scale = __uint_as_float(top) / 127.f;
     if (!(scale > 0.f)) scale = 1.f;   // all zero (or so small that a scale would be): whole numbers are zero
     if (tid == 0) a.scale[row] = bad ? __builtin_nanf("") : scale;
+    // x / scale by the scale's reciprocal and one step for what is left, which rounds as a division does, in a third of its instructions;
+    // scales whose reciprocal is near the ends of the range are divided by
+    const float inv = 1.f / scale;
+    const bool plain = scale > 0x1p-100f && scale < 0x1p100f;
     auto put = [&](int c, const float *x) {
         uint32_t w[2] = {0, 0};
         if (!bad)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e >> 2] |= ((uint32_t)(int)rintf(x[e] / scale) & 0xFFu) << (8 * (e & 3));
+            for (int e = 0; e < 8; ++e) {
+                const float q = x[e] * inv, d = plain ? __builtin_fmaf(__builtin_fmaf(-q, scale, x[e]), inv, q) : x[e] / scale;
+                w[e >> 2] |= ((uint32_t)(int)rintf(d) & 0xFFu) << (8 * (e & 3));
+            }
         *(u32x2 *)(a.q + row * a.ldq + 8 * c) = (u32x2){w[0], w[1]};
     };
     if (CH > 0)
@@ -241,13 +252,13 @@ __device__ __forceinline__ void finish4(const LinearArgs &a, int m, int n, i32x4
 }
 
 // Up to 64 rows: the weights stream.  A workgroup owns U groups of 16 output channels; its eight waves take chunks of KC terms in turn.  A
-// wave asks memory for whole runs of a channel or row, KC bytes at a time: reading an operand as the matrix pipe wants it, 64 bytes of
+// wave asks memory for runs of a channel or row, KC bytes at a time: reading an operand as the matrix pipe wants it, 64 bytes of
 // 16 channels an instruction, streams 4.4 to 5.1 TB/s here, runs of 1 KiB 6.2.  It turns a tile (16 rows or channels of a chunk) into
 // operands through LDS of its own (no barrier; 16-byte pieces at their place XOR the row's number).  A chunk is MT tiles of the rows,
 // kept as operands, and U of the weights; AHEAD tiles are under way in registers.
-template <int U, int MT, int KC, int AHEAD>
+template <int U, int MT, int AHEAD>
 __global__ __launch_bounds__(512) void k_linear_rows(LinearArgs a) {
-    constexpr int NW = 8, KS = KC / 64, LD = KC / 64, V = U + MT;   // LD: loads a tile is
+    constexpr int KC = 256, NW = 8, KS = KC / 64, LD = KC / 64, V = U + MT;   // LD: loads a tile is
     constexpr int LPR = KC / 16, RPL = 64 / LPR;                    // lanes of a run, runs of a load
     constexpr size_t TURN = (size_t)NW * 16 * KC, RED = (size_t)(NW / 2) * U * MT * 1024;
     static_assert(V % AHEAD == 0, "a tile's registers are the same in every chunk");
@@ -324,12 +335,12 @@ __global__ __launch_bounds__(512) void k_linear_rows(LinearArgs a) {
     }
 }
 
-// More rows: tiles of BM rows by BN channels through LDS, four waves of 16 TM rows by 16 TN channels each; 128 terms at a time, the next
+// More rows: tiles of BM rows by BN channels through LDS, WM x WN waves of 16 TM rows by 16 TN channels each; 128 terms at a time, the next
 // ones on their way into registers while these are multiplied.  A row's 16-byte pieces are stored at their place XOR the row's number
 // modulo 8: a wave's reads of 16 rows then meet different banks.
-template <int TM, int TN>
-__global__ __launch_bounds__(256) void k_linear_tiles(LinearArgs a) {
-    constexpr int BM = 32 * TM, BN = 32 * TN, LX = BM / 32, LW = BN / 32;   // 16-byte loads a thread
+template <int TM, int TN, int WM, int WN, int AHEAD>
+__global__ __launch_bounds__(64 * WM * WN) void k_linear_tiles(LinearArgs a) {
+    constexpr int NT = 64 * WM * WN, RPT = NT / 8, BM = 16 * TM * WM, BN = 16 * TN * WN, LX = BM / RPT, LW = BN / RPT;   // 16-byte loads a thread
     __shared__ __attribute__((aligned(16))) int8_t sx[2][BM * 128], sw[2][BN * 128];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
     const int nm = (a.rows + BM - 1) / BM, nn = (a.out + BN - 1) / BN, total = nm * nn * a.splits;
@@ -343,51 +354,57 @@ __global__ __launch_bounds__(256) void k_linear_tiles(LinearArgs a) {
     const int ldw = (int)a.ldw, ldq = (int)a.ldq;
     const rsrc_t wr = rows_from(a.w, a.ldw, n0, a.out, a.in), xr = rows_from(a.q, a.ldq, m0, a.rows, a.in);
     const unsigned w_lane = row * ldw + 16 * piece, x_lane = row * ldq + 16 * piece;
-    i32x4 rx[LX], rw[LW];
-    auto load = [&](int c) {   // past a row's end: any weights, times zero
+    i32x4 rx[AHEAD][LX], rw[AHEAD][LW];
+    auto load = [&](int slot, int c) {   // past the last chunk nothing; past a row's end zeros for the rows, whatever there is for the weights
         const int k = c * 128;
-        const unsigned at = k + 16 * piece < a.in ? x_lane : OUTSIDE;
+        const unsigned xa = c < c1 && k + 16 * piece < a.in ? x_lane + k : OUTSIDE, wa = c < c1 ? w_lane + k : OUTSIDE;
 #pragma unroll
-        for (int i = 0; i < LX; ++i) rx[i] = load16(xr, at, 32 * i * ldq + k);
+        for (int i = 0; i < LX; ++i) rx[slot][i] = load16(xr, xa, RPT * i * ldq);
 #pragma unroll
-        for (int i = 0; i < LW; ++i) rw[i] = load16(wr, w_lane, 32 * i * ldw + k);
+        for (int i = 0; i < LW; ++i) rw[slot][i] = load16(wr, wa, RPT * i * ldw);
     };
-    auto store = [&](int slot) {
+    auto store = [&](int slot, int half) {
 #pragma unroll
-        for (int i = 0; i < LX; ++i) *(i32x4 *)(sx[slot] + put + 32 * 128 * i) = rx[i];
+        for (int i = 0; i < LX; ++i) *(i32x4 *)(sx[half] + put + RPT * 128 * i) = rx[slot][i];
 #pragma unroll
-        for (int i = 0; i < LW; ++i) *(i32x4 *)(sw[slot] + put + 32 * 128 * i) = rw[i];
+        for (int i = 0; i < LW; ++i) *(i32x4 *)(sw[half] + put + RPT * 128 * i) = rw[slot][i];
     };
     i32x4 acc[TN][TM];
 #pragma unroll
     for (int n = 0; n < TN; ++n)
 #pragma unroll
         for (int m = 0; m < TM; ++m) acc[n][m] = (i32x4){0, 0, 0, 0};
-    const int wm = (wave & 1) * 16 * TM, wn = (wave >> 1) * 16 * TN;
-    if (c0 < c1) {
-        load(c0);
-        store(0);
-    }
-    __syncthreads();
-    for (int c = c0; c < c1; ++c) {
-        const int slot = (c - c0) & 1;
-        if (c + 1 < c1) load(c + 1);
+    const int wm = wave % WM * 16 * TM, wn = wave / WM * 16 * TN;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int at = ((4 * s + lg) ^ (li & 7)) << 4;
-            i32x4 x[TM], w[TN];
+    for (int u = 0; u < AHEAD; ++u) load(u, c0 + u);
+    store(0, 0);
+    int half = 0;
+    // loads AHEAD chunks ahead; the barrier waits for LDS alone, so that they stay under way
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    for (int cc = c0; cc < c1; cc += AHEAD)
 #pragma unroll
-            for (int m = 0; m < TM; ++m) x[m] = *(const i32x4 *)(sx[slot] + (wm + 16 * m + li) * 128 + at);
+        for (int u = 0; u < AHEAD; ++u) {
+            const int c = cc + u;
+            load(u, c + AHEAD);
+            if (c < c1) {
 #pragma unroll
-            for (int n = 0; n < TN; ++n) w[n] = *(const i32x4 *)(sw[slot] + (wn + 16 * n + li) * 128 + at);
+                for (int s = 0; s < 2; ++s) {
+                    const int at = ((4 * s + lg) ^ (li & 7)) << 4;
+                    i32x4 x[TM], w[TN];
 #pragma unroll
-            for (int n = 0; n < TN; ++n)
+                    for (int m = 0; m < TM; ++m) x[m] = *(const i32x4 *)(sx[half] + (wm + 16 * m + li) * 128 + at);
 #pragma unroll
-                for (int m = 0; m < TM; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[n], x[m], acc[n][m], 0, 0, 0);
+                    for (int n = 0; n < TN; ++n) w[n] = *(const i32x4 *)(sw[half] + (wn + 16 * n + li) * 128 + at);
+#pragma unroll
+                    for (int n = 0; n < TN; ++n)
+#pragma unroll
+                        for (int m = 0; m < TM; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[n], x[m], acc[n][m], 0, 0, 0);
+                }
+                half ^= 1;
+                store((u + 1) % AHEAD, half);
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            }
         }
-        if (c + 1 < c1) store(slot ^ 1);
-        __syncthreads();
-    }
     const int ldp = (a.out + 3) / 4 * 4;
 #pragma unroll
     for (int n = 0; n < TN; ++n)
@@ -423,17 +440,23 @@ template <int FORM, bool F32> void quantize(hipStream_t st, const QuantArgs &a, 
 }
 
 struct Plan {
-    int tile;     // 0: row groups; else the tiles' form
-    int units;    // row groups: groups of 16 channels a workgroup
-    int splits;
+    enum Form { ROWS, TILE128, TILE256 } form;
+    int units;    // ROWS: groups of 16 channels a workgroup
+    int splits;   // of the terms
 };
+// The launch that takes the least time by what each form takes on 256 compute units (us, measured at 4096 to 17920 terms):
+// Row groups, up to 64 rows: a round of compute units takes as long as a workgroup's channels, and as one group more for its beginning
+// and end.  26 x 22016 x 4096 with 1, 2, 3, 4, 6, 8 groups: 26.1, 24.0, 23.0, 25.9, 23.5, 23.9; 60 x 12288: 23.7, 21.1, 16.5, 17.1, 22.6, 27.2.
+// Tiles: a compute unit takes 0.72 a chunk of 128 terms of a tile of 128 x 128 (two of which run side by side) and 2.0 of one of 256 x 256, and
+// 1.5 and 6 for a tile's beginning and end; splitting the terms costs a second launch and the partial sums' way there and back.
+// 2000 x 22016 x 4096: 274 (128), 222 (256); 480 x 35840 x 6656: 170, 214; 480 x 6656 x 17920 with 1, 2, 4 splits: 105, 95, 105 and 249, 137, 88.
 Plan plan_of(int rows, int out, int in) {
-    Plan p{0, 1, 1};
+    Plan p{Plan::ROWS, 1, 1};
     if (rows <= 64) {
         const int groups = (out + 15) / 16;
         int best = 0x7FFFFFFF;
         for (int u : {1, 2, 3, 4, 6, 8}) {
-            if (u == 8 && rows > 32) continue;
+            if (u == 8 && rows > 32) continue;   // no registers for it
             const int wgs = (groups + u - 1) / u, cost = (wgs + 255) / 256 * (u + 1);
             if (cost <= best) {
                 best = cost;
@@ -442,39 +465,51 @@ Plan plan_of(int rows, int out, int in) {
         }
         return p;
     }
-    const char *e = getenv("TILE"), *sp = getenv("SPL");
-    p.tile = e ? atoi(e) : 1;
-    p.splits = sp ? atoi(sp) : 1;
+    double best = 1e30;
+    const int chunks = (in + 127) / 128;
+    for (Plan::Form f : {Plan::TILE128, Plan::TILE256}) {
+        const int side = f == Plan::TILE128 ? 128 : 256;
+        const double tiles = (double)((rows + side - 1) / side) * ((out + side - 1) / side);
+        if (tiles * 16 > 2147483647.0) continue;
+        for (int s = 1; s <= 16 && s <= chunks; ++s) {
+            const double each = (chunks + s - 1) / s * (f == Plan::TILE128 ? 0.72 : 2.0) + (f == Plan::TILE128 ? 1.5 : 6.0);
+            const double us = std::ceil(tiles * s / 256) * each + (s > 1 ? 4.0 + (double)s * rows * out * 8 / 1e7 : 0.0);
+            if (us < best) {
+                best = us;
+                p.form = f;
+                p.splits = s;
+            }
+        }
+    }
     return p;
 }
 
-template <int U, int MT, int KC, int AHEAD> void rows_launch(hipStream_t st, const LinearArgs &a) {
-    k_linear_rows<U, MT, KC, AHEAD><<<dim3((a.out + 16 * U - 1) / (16 * U), (a.rows + 16 * MT - 1) / (16 * MT)), 512, 0, st>>>(a);
+template <int U, int MT, int AHEAD> void rows_launch(hipStream_t st, const LinearArgs &a) {
+    k_linear_rows<U, MT, AHEAD><<<dim3((a.out + 16 * U - 1) / (16 * U), (a.rows + 16 * MT - 1) / (16 * MT)), 512, 0, st>>>(a);
 }
 template <int MT> void rows_by_units(hipStream_t st, const LinearArgs &a, int units) {
     switch (units) {
-    case 1: rows_launch<1, MT, MT == 4 ? 256 : KCS, 1 + MT>(st, a); break;
-    case 2: rows_launch<2, MT, MT == 4 ? 256 : KCS, MT == 1 ? 3 : MT == 2 ? 4 : 3>(st, a); break;
-    case 3: rows_launch<3, MT, 256, MT == 1 ? 4 : MT == 2 ? 5 : 7>(st, a); break;
-    case 4: rows_launch<4, MT, 256, MT == 1 ? 5 : MT == 2 ? 6 : 4>(st, a); break;
-    case 6: rows_launch<6, MT, 256, MT == 1 ? 7 : MT == 2 ? 4 : 5>(st, a); break;
-    default: if constexpr (MT < 4) rows_launch<8, MT, 256, MT == 1 ? 3 : 5>(st, a); break;
+    case 1: rows_launch<1, MT, 1 + MT>(st, a); break;
+    case 2: rows_launch<2, MT, MT == 1 ? 3 : MT == 2 ? 4 : 3>(st, a); break;
+    case 3: rows_launch<3, MT, MT == 1 ? 4 : MT == 2 ? 5 : 7>(st, a); break;
+    case 4: rows_launch<4, MT, MT == 1 ? 5 : MT == 2 ? 6 : 4>(st, a); break;
+    case 6: rows_launch<6, MT, MT == 1 ? 7 : MT == 2 ? 4 : 5>(st, a); break;
+    default: if constexpr (MT < 4) rows_launch<8, MT, MT == 1 ? 3 : 5>(st, a); break;
     }
 }
-template <int TM, int TN> void tiles_launch(hipStream_t st, const LinearArgs &a) {
-    k_linear_tiles<TM, TN><<<(a.rows + 32 * TM - 1) / (32 * TM) * ((a.out + 32 * TN - 1) / (32 * TN)) * a.splits, 256, 0, st>>>(a);
+template <int TM, int TN, int WM, int WN, int AHEAD> void tiles_launch(hipStream_t st, const LinearArgs &a) {
+    constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN;
+    k_linear_tiles<TM, TN, WM, WN, AHEAD><<<(a.rows + BM - 1) / BM * ((a.out + BN - 1) / BN) * a.splits, 64 * WM * WN, 0, st>>>(a);
 }
 void launch_linear(hipStream_t st, const LinearArgs &a, const Plan &p) {
-    switch (p.tile) {
-    case 0:
+    if (p.form == Plan::ROWS) {
         if (a.rows <= 16) rows_by_units<1>(st, a, p.units);
         else if (a.rows <= 32) rows_by_units<2>(st, a, p.units);
         else rows_by_units<4>(st, a, p.units);
         return;
-    case 1: tiles_launch<4, 4>(st, a); break;
-    case 2: tiles_launch<8, 4>(st, a); break;
-    case 3: tiles_launch<4, 8>(st, a); break;
     }
+    if (p.form == Plan::TILE128) tiles_launch<4, 4, 2, 2, 3>(st, a);
+    else tiles_launch<8, 4, 2, 4, 2>(st, a);
     if (a.splits > 1) k_linear_join<<<(unsigned)(((size_t)a.rows * ((a.out + 3) / 4) + 255) / 256), 256, 0, st>>>(a);
 }
 

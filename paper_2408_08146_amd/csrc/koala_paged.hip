@@ -112,6 +112,7 @@ template <int DH, bool F32> __global__ __launch_bounds__(256) void k_paged_appen
     if (row_ >= (unsigned)a.rows) return;
     const int row = (int)row_, u = (int)(at - row_ * per_row), hs = u / LPH, j = u % LPH;
     const int b = row / a.rows_per_seq, i = row - b * a.rows_per_seq;
+    if (a.n_new && i >= a.n_new[b]) return;
     const bool is_q = hs < a.n_heads, is_k = !is_q && hs < a.n_heads + a.p.n_kv;
     const int h = is_q ? hs : is_k ? hs - a.n_heads : hs - a.n_heads - a.p.n_kv;
     const void *src = is_q ? a.q : is_k ? a.k : a.v;
@@ -121,7 +122,7 @@ template <int DH, bool F32> __global__ __launch_bounds__(256) void k_paged_appen
     load8<F32>(src, from + DH / 2, x[1]);
     const int ctx = a.ctx_len[b], slot = ctx + i, pos = ctx + (a.depth ? a.depth[i] : i);
     // (slots of a negative length are outside the table)
-    if ((a.n_new && i >= a.n_new[b]) || ctx < 0 || pos < 0 || pos >= a.rope_rows) return;
+    if (ctx < 0 || pos < 0 || pos >= a.rope_rows) return;
     if (is_q || is_k) {
         float c[8], s[8];
         load8<true>(a.cos, (size_t)pos * (DH / 2) + 8 * j, c);
@@ -222,7 +223,7 @@ template <int DH> __global__ __launch_bounds__(256) void k_paged_commit(CommitAr
     if (a.new_len && layer == 0 && h == 0 && j == 0) a.new_len[b] = ctx + a.accept_len[b] + 1;
     const size_t base = layer * a.p.layer_rows + ((size_t)h << a.p.log_page);
     constexpr int AHEAD = 8;
-    for (int i0 = 1; i0 <= n; i0 += AHEAD) {
+    for (int i0 = 1; i0 == 1 || i0 <= n; i0 += AHEAD) {
         u32x4 x[AHEAD];
         uint32_t e[AHEAD];
         long to[AHEAD];
@@ -230,9 +231,9 @@ template <int DH> __global__ __launch_bounds__(256) void k_paged_commit(CommitAr
         for (int z = 0; z < AHEAD; ++z) {
             const int i = i0 + z;
             to[z] = -1;
-            if (i > n) continue;
-            const int node = a.accept_path[(size_t)b * a.path_stride + i];
-            if (node <= i || ctx < 0) continue;   // in its place already (or none)
+            if (i >= a.path_stride) continue;
+            const int node = a.accept_path[(size_t)b * a.path_stride + i];   // (asked for beside the lengths, not after them)
+            if (i > n || node <= i || ctx < 0) continue;                      // none, or in its place already
             const long s = slot_row(a.p, b, ctx + node), d = slot_row(a.p, b, ctx + i);
             if (s < 0 || d < 0) continue;
             to[z] = (long)base + d;
