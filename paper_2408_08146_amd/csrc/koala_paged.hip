@@ -283,6 +283,7 @@ constexpr int WAVES = 4, STEP = 32;   // of a workgroup that shares items with o
 constexpr int PER_ITEM = 24;
 constexpr int MAX_PARTS = 32;   // workgroups an item is spread over, on average at most
 constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LAG = 8.f, HALF_SHIFT = 4.f;   // in powers of two
 // block exponents (plus 127) whose values fp16 holds exactly: 1/2 2^-23 is its smallest, 6 2^13 below its largest
 constexpr unsigned HALF_LO = 127 - 23, HALF_HI = 127 + 13;
 
@@ -291,12 +292,6 @@ __device__ __forceinline__ float lane_groups_max(float x) {
     x = fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float lane_groups_sum(float x) {
-    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(q[0]) + __uint_as_float(q[1]);
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 // eight values as the sum of N bfloat16 pieces, each the rounding of what the ones before it leave
 template <int N> __device__ __forceinline__ void split8(const float *y, bf16x8 *piece) {
@@ -330,7 +325,6 @@ template <int CW> struct Codes {
     words<CW> k[2], v[2];
     unsigned ke[2], ve[2];
 };
-__device__ __forceinline__ float block_scale(unsigned e) { return e == NAN_EXP ? __builtin_nanf("") : exp_scale(e); }
 __device__ __forceinline__ f16x8 decode8h(uint32_t c, float s) {
     const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 1),
                 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 3);
@@ -399,7 +393,7 @@ constexpr int ahead(int MT, bool F32) { return MT == 2 ? 3 : F32 ? 2 : 3; }
 
 // WHOLE: every item is one workgroup's, of eight waves; the grid is the items
 template <int DH, int MT, bool F32, bool WHOLE>
-__global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, MT == 2 || F32 || WHOLE ? 2 : 3) void k_paged_attend(AttendArgs a) {
+__global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, 2) void k_paged_attend(AttendArgs a) {
     constexpr int NW = WHOLE ? 8 : WAVES;
     constexpr int KS = DH / 32, DT = DH / 16, NQ = F32 ? 3 : 1;   // bfloat16 pieces of queries
     constexpr int VS = DH * 2 + 32;        // bytes of a value row in LDS: a transposing load's 16 lanes hit different banks
@@ -476,37 +470,38 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, MT == 2 || F32 || WHOLE ?
             }
         }
         if (QLDS) __syncthreads();
-        f32x4 acc[MT][DT];
-        float m_run[MT], l_run[MT];
+        f32x4 acc[MT][DT + 1];   // the last: the weights' sum, a product with ones, in every register of it
+        float m_run[MT];
         auto reset = [&]() {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 m_run[mt] = -INFINITY;
-                l_run[mt] = 0.f;
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) acc[mt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                for (int dt = 0; dt <= DT; ++dt) acc[mt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
             }
         };
         reset();
         const int32_t *table = a.p.table + (size_t)b * a.p.pages_per_seq;
         const int last_key = max(kv_end - 1, 0), place = (1 << a.p.log_page) - 1, last = s0 + n;
-        // the wave's steps are s0 + wave + NW * i; steps past the last one are asked for as the last
+        // The wave's steps are s0 + wave + NW * i; steps past the last one are asked for as the last.  The 16 keys of half a step are in one
+        // page (of 16 slots at least), so their place is a scalar's business; keys past the end are the page's other slots.
+        auto first_key = [&](int st, int j) { return min(min(st, last - 1) * STEP + 16 * j, last_key & ~15); };
         auto find = [&](int *page, int st) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) page[j] = table[min(min(st, last - 1) * STEP + 16 * j + li, last_key) >> a.p.log_page];
+            for (int j = 0; j < 2; ++j) page[j] = table[first_key(st, j) >> a.p.log_page];
         };
+        const unsigned lane_codes = li * (DH / 2) + lg * (4 * CW), lane_exps = li * (DH / BLOCK) + (DH == 128 ? lg : lg >> 1);
         auto fetch = [&](Codes<CW> &c, const int *page, int st) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int key = min(min(st, last - 1) * STEP + 16 * j + li, last_key);
                 // a page number outside the pool is the caller's mistake; it is kept from being an address outside of it
-                const unsigned pg = (unsigned)page[j] < (unsigned)a.p.n_pages ? (unsigned)page[j] : 0u;
-                const size_t r = (((size_t)pg * a.p.n_kv + h) << a.p.log_page) + (key & place);
-                const size_t o = r * (DH / 2) + lg * (4 * CW), e = r * (DH / BLOCK) + (DH == 128 ? lg : lg >> 1);
-                c.k[j] = *(const words<CW> *)(a.p.k + o);
-                c.v[j] = *(const words<CW> *)(a.p.v + o);
-                c.ke[j] = a.p.ks[e];
-                c.ve[j] = a.p.vs[e];
+                unsigned pg = (unsigned)__builtin_amdgcn_readfirstlane(page[j]);
+                pg = pg < (unsigned)a.p.n_pages ? pg : 0u;
+                const size_t r = (((size_t)pg * a.p.n_kv + h) << a.p.log_page) + (first_key(st, j) & place);
+                c.k[j] = *(const words<CW> *)(a.p.k + r * (DH / 2) + lane_codes);
+                c.v[j] = *(const words<CW> *)(a.p.v + r * (DH / 2) + lane_codes);
+                c.ke[j] = *(a.p.ks + r * (DH / BLOCK) + lane_exps);
+                c.ve[j] = *(a.p.vs + r * (DH / BLOCK) + lane_exps);
             }
         };
         // S^T = K Q^T
@@ -515,7 +510,7 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, MT == 2 || F32 || WHOLE ?
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) sc[j][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-                const float s = block_scale(c.ke[j]);
+                const float s = exp_scale(c.ke[j]);   // (255: the conversion gives not-a-number, whatever the code)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
                     const bf16x8 kf = decode8(c.k[j][ks], s);
@@ -529,27 +524,38 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, MT == 2 || F32 || WHOLE ?
                 }
             }
         };
-        // With M the largest score so far times `scale`, a weight is 2^(score * scale - M), one multiply-add and one power; for fp16
-        // it is 2^8 of that, so that weights down to 2^-22 of the largest have all their bits.
-        auto weights = [&](int mt, float *p) {
-            float top = p[0], sum = 0.f;
+        // A weight is 2^(score * scale - M), one multiply-add and one power, where M is the largest score * scale when it was last looked up:
+        // it moves, and the sums with it, only where a larger one is past it by more than LAG (a wave of 16 rows meets a new maximum of some
+        // row in most of its steps, one that far off hardly ever).  Weights are at most 2^LAG; for fp16 they are 2^HALF_SHIFT of that, so that
+        // those down to 2^-18 have all their bits.
+        auto maxima = [&](const float (*p)[8], float *shift) {
+            float m_new[MT];
+            bool moved = false;
 #pragma unroll
-            for (int e = 1; e < 8; ++e) top = fmaxf(top, p[e]);
-            const float m_new = fmaxf(m_run[mt], lane_groups_max(top) * a.scale);
-            const float m_use = m_new == -INFINITY ? 0.f : m_new;   // nothing seen so far: 2^(-inf), not 2^(-inf + inf)
-            const float alpha = __builtin_amdgcn_exp2f(m_run[mt] - m_use);
-            const float shift = (F32 ? 0.f : 8.f) - m_use;
+            for (int mt = 0; mt < MT; ++mt) {
+                float top = p[mt][0];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], a.scale, shift));
-                sum += p[e];
+                for (int e = 1; e < 8; ++e) top = fmaxf(top, p[mt][e]);
+                top = lane_groups_max(top) * a.scale;
+                m_new[mt] = top > m_run[mt] + LAG ? top : m_run[mt];
+                moved |= m_new[mt] != m_run[mt];
             }
-            m_run[mt] = m_new;
-            l_run[mt] = l_run[mt] * alpha + sum;
-            if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
+            if (__builtin_amdgcn_ballot_w64(moved) != 0) {
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) acc[mt][dt] *= alpha;
+                for (int mt = 0; mt < MT; ++mt) {
+                    const float alpha = m_new[mt] == m_run[mt] ? 1.f : __builtin_amdgcn_exp2f(m_run[mt] - m_new[mt]);
+#pragma unroll
+                    for (int dt = 0; dt <= DT; ++dt) acc[mt][dt] *= alpha;
+                    m_run[mt] = m_new[mt];
+                }
             }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)   // nothing seen so far: 2^(-inf), not 2^(-inf + inf)
+                shift[mt] = (F32 ? 0.f : HALF_SHIFT) - (m_run[mt] == -INFINITY ? 0.f : m_run[mt]);
+        };
+        auto powers = [&](float *p, float shift) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], a.scale, shift));
         };
         // O^T += V^T P^T; slot (lane group g, element e) of the contraction is key 16 (e / 4) + 4 g + e % 4, which is where the scores
         // lie.  Transposing load: lane i of 16 points at key row 4 g + i / 4, columns 16 dt + 4 (i % 4) .. and gets keys 4 g .. 4 g + 3
@@ -565,8 +571,8 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, MT == 2 || F32 || WHOLE ?
             bf16x8 pf[3];
             split8<3>(p, pf);
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                const bf16x8 va = values(dt);
+            for (int dt = 0; dt <= DT; ++dt) {
+                const bf16x8 va = dt < DT ? values(dt) : (bf16x8){1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
 #pragma unroll
                 for (int z = 0; z < 3; ++z) acc[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf[z], acc[mt][dt], 0, 0, 0);
             }
@@ -597,44 +603,52 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, MT == 2 || F32 || WHOLE ?
 #pragma unroll
                 for (int i = 0; i < CW; ++i) *(u32x4_alias *)(put + 16 * j * VS + 16 * i) = __builtin_bit_cast(u32x4, decode8(drop ? 0u : c.v[j][i], s));
             }
+            float p[MT][8], shift[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                float p[8];
                 const uint32_t mine = seen[mt] >> (4 * lg);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = (mine >> (16 * (e >> 2) + (e & 3))) & 1u ? sc[e >> 2][mt][e & 3] : -INFINITY;
-                weights(mt, p);
-                exact_product(mt, p);
+                for (int e = 0; e < 8; ++e) p[mt][e] = (mine >> (16 * (e >> 2) + (e & 3))) & 1u ? sc[e >> 2][mt][e & 3] : -INFINITY;
+            }
+            maxima(p, shift);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                powers(p[mt], shift[mt]);
+                exact_product(mt, p[mt]);
             }
         };
-        // A step whose keys every row sees; V and P in fp16 where the output is bfloat16
+        // A step whose keys every row sees, its scores there already; V and P in fp16 where the output is bfloat16.  The next step's scores
+        // are taken beside this one's powers and products: neither waits for the other.
         unsigned beyond = 0;   // whether a value was outside fp16's range: then it is all done again
-        auto full_step = [&](const Codes<CW> &c) {
-            f32x4 sc[2][MT];
-            scores(c, sc);
+        f32x4 sc[2][MT];
+        auto full_step = [&](const Codes<CW> &c, const Codes<CW> &next) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float s = block_scale(c.ve[j]);
+                const float s = exp_scale(c.ve[j]);
                 if (!F32) beyond |= c.ve[j] - HALF_LO > HALF_HI - HALF_LO;
 #pragma unroll
                 for (int i = 0; i < CW; ++i)
                     *(u32x4_alias *)(put + 16 * j * VS + 16 * i) =
                         F32 ? __builtin_bit_cast(u32x4, decode8(c.v[j][i], s)) : __builtin_bit_cast(u32x4, decode8h(c.v[j][i], s));
             }
+            float p[MT][8], shift[MT];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[mt][e] = sc[e >> 2][mt][e & 3];
+            maxima(p, shift);
+            scores(next, sc);
             f16x8 ph[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                float p[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = sc[e >> 2][mt][e & 3];
-                weights(mt, p);
-                if (F32) exact_product(mt, p);
-                else ph[mt] = __builtin_convertvector((f32x8){p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]}, f16x8);
+                powers(p[mt], shift[mt]);
+                if (F32) exact_product(mt, p[mt]);
+                else ph[mt] = __builtin_convertvector((f32x8){p[mt][0], p[mt][1], p[mt][2], p[mt][3], p[mt][4], p[mt][5], p[mt][6], p[mt][7]}, f16x8);
             }
             if (!F32)
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    const f16x8 va = __builtin_bit_cast(f16x8, values(dt));
+                for (int dt = 0; dt <= DT; ++dt) {
+                    const f16x8 va = dt < DT ? __builtin_bit_cast(f16x8, values(dt)) : (f16x8){1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) acc[mt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ph[mt], acc[mt][dt], 0, 0, 0);
                 }
@@ -654,10 +668,11 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, MT == 2 || F32 || WHOLE ?
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) fetch(c[u], page[u], st + u * NW);
             if (open < mine) any_step(c_end, st + (mine - 1) * NW);
+            scores(c[0], sc);
             for (int i = 0; i < open; i += AHEAD)
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u) {
-                    if (i + u < open) full_step(c[u]);
+                    if (i + u < open) full_step(c[u], c[(u + 1) % AHEAD]);
                     fetch(c[u], page[AHEAD], st + (i + u + AHEAD) * NW);
                     find(page[AHEAD], st + (i + u + AHEAD + 1) * NW);
                 }
@@ -682,13 +697,12 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, MT == 2 || F32 || WHOLE ?
                     if ((nan_v[mt] >> (dt * 64 / DH)) & 1)
                         acc[mt][dt] = (f32x4){__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
             }
-            const float lsum = lane_groups_sum(l_run[mt]);
             __syncthreads();
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) mo[(wave * DT + dt) * 64 + l] = acc[mt][dt];
             if (lg == 0) {
                 mm[wave][li][0] = m_run[mt];
-                mm[wave][li][1] = lsum;
+                mm[wave][li][1] = acc[mt][DT][0];
             }
             __syncthreads();
             float M = -INFINITY, L = 0.f, f[NW];
@@ -830,8 +844,6 @@ koala_status launched() { return hipGetLastError() == hipSuccess ? KOALA_OK : KO
 // workgroups of 256 for n lanes; 0 if the lanes cannot be counted in 32 bits
 unsigned blocks_of(size_t n) { return n > 0xFFFFFF00ull ? 0 : (unsigned)((n + 255) / 256); }
 
-// row tiles of an attention item (the pieces of fp32 queries leave no registers for a second)
-int tiles_of(int rows, bool f32) { return rows <= 16 || f32 ? 1 : 2; }
 int attend_wgs(int cu) { return 2 * cu; }
 int compute_units() {
     static const int n = [] {
@@ -843,8 +855,12 @@ int compute_units() {
 }
 enum { ATTEND_WGS_MAX = 512 };   // what the workspace is sized for
 
-// Whether every item is left to one workgroup, which spares the second launch.  (us)
-bool attend_whole(int items, int steps, int cu) { return items <= cu ? steps <= 80 : steps <= 16; }
+// Whether every item is left to one workgroup, which spares the second launch and the parts' way through memory: where all items run at
+// once, until dividing them among the idle compute units pays.  us whole and divided, heads of 128, over 500, 1000, 2000, 3000, 4000 keys:
+// 32 items of one row 8.2, 9.5, 13.6, 17.3, 21.1 and 11.7, 12.2, 14.0, 14.2, 14.3; 64 items (26 rows) 8.4, 10.2, 14.4, 18.0, 22.0 and 14.4, 16.0,
+// 17.9, 18.7, 20.0; 240 items (26 rows) 8.5, 11.3, 18.6, 20.8, 26.1 and 17.4, 19.2, 21.5, 24.9, 27.2.  In more than one round only small items: 280
+// over 600, 1000, 3000 keys 13.6, 18.7, 36.3 and 15.4, 18.3, 28.0; 1200 35.8, 47.5, 104.5 and 35.3, 41.9, 97.3.
+bool attend_whole(int items, int steps, int cu) { return items <= cu ? steps <= 60 + items / 2 : items <= 4 * cu && steps <= 16; }
 
 template <int DH, int MT, bool F32>
 void launch_attend(hipStream_t st, const AttendArgs &a, int cu) {
@@ -965,17 +981,18 @@ koala_status koala_paged_attend(const koala_paged_kv *kv, void *hip_stream, int 
     size_t need = 0;
     (void)koala_paged_workspace_bytes(kv, &need);
     if (workspace_bytes < need) return KOALA_E_WORKSPACE;
-    const int MT = tiles_of(rows * (n_heads / KV), dtype == KOALA_FP32);
     AttendArgs a{};
     a.p = pool_of(kv, layer);
     a.ctx_len = kv->ctx_len; a.mask = mask; a.mask_stride = (size_t)mask_stride;
     a.batch = batch; a.rows = rows; a.n_heads = n_heads;
-    a.groups = (rows * (n_heads / KV) + MT * 16 - 1) / (MT * 16);
     a.scale = scale * LOG2E;
-    const int room = kv->pages_per_seq * kv->page_size;
+    const int room = kv->pages_per_seq * kv->page_size, cu = compute_units(), tiles = (rows * (n_heads / KV) + 15) / 16;
     a.max_len = max_len > 0 && max_len < room ? max_len : room;
+    // One row tile an item where there is only one, where the pieces of fp32 queries leave no registers for a second, and where all items
+    // are one workgroup's and run at once.
+    const int MT = tiles == 1 || dtype == KOALA_FP32 || ((double)batch * KV * tiles <= cu && attend_whole(batch * KV * tiles, a.max_len / STEP, cu)) ? 1 : 2;
+    a.groups = (tiles + MT - 1) / MT;
     if ((double)batch * KV * a.groups * (a.max_len / STEP + 1 + PER_ITEM) > 2147483647.0) return KOALA_E_SHAPE;   // steps are counted in 32 bits
-    const int cu = compute_units();
     a.wgs = attend_wgs(cu);
     if (a.wgs > ATTEND_WGS_MAX) a.wgs = ATTEND_WGS_MAX;
     a.q = q; a.ldq = (size_t)q_stride; a.out = out;
