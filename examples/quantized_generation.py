@@ -1,0 +1,214 @@
+"""Draft-then-verify generation with a target in 8-bit projections over a 4-bit paged cache.
+
+The draft head and the acceptance walk are the library's (KoalaContext); verification runs here, layer by layer: RMSNorm and
+quantiser, integer QKV product, rotation and append, attention over the pages, integer products back into the residual stream.
+A verification is captured once in a graph and replayed; the accepted path's rows are committed in the pages.
+
+    python examples/quantized_generation.py            # a small predictable pair: what is generated, tokens per iteration
+    python examples/quantized_generation.py --time     # 7B shape, random weights: time of a verification beside the 16-bit path's
+"""
+from __future__ import annotations
+
+import argparse
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+import paper_2408_08146_amd as koala  # noqa: E402
+from koala_synth import get_config, make_tree, predictable_pair  # noqa: E402
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+class QuantizedTarget:
+    """A Llama-style target: int8 weights with a scale per output channel, activations quantised per token, keys and values in 4 bits.
+
+    weight(name) gives a matrix or gain on the device by the names of koala_synth (`layers.0.wq`, ...); `rows` is the most a call
+    takes per sequence (64 at most)."""
+
+    def __init__(self, cfg, weight, batch, capacity, rows=64, page=64):
+        self.cfg, self.batch, self.rows = cfg, batch, rows
+        H, F, V, heads, dh, L = (cfg[k] for k in ("hidden", "ffn", "vocab", "n_heads", "head_dim", "n_layers"))
+        linear = lambda w: koala.QuantizedLinear(*koala.quantize_weight(w))
+        gate_up = lambda l: torch.stack((weight(f"layers.{l}.wgate"), weight(f"layers.{l}.wup")), 1).reshape(2 * F, H)
+        self.embed = weight("embed")
+        self.layers = [dict(in_norm=weight(f"layers.{l}.in_norm"), post_norm=weight(f"layers.{l}.post_norm"),
+                            qkv=linear(torch.cat([weight(f"layers.{l}.{n}") for n in ("wq", "wk", "wv")])),
+                            o=linear(weight(f"layers.{l}.wo")), gate_up=linear(gate_up(l)), down=linear(weight(f"layers.{l}.wdown")))
+                       for l in range(L)]
+        self.final_norm, self.head = weight("final_norm"), linear(weight("lm_head"))
+        pages = -(-capacity // page)
+        pools = koala.alloc_paged_cache(L, batch * pages, page, heads, dh)
+        order = torch.randperm(batch * pages, device="cuda").int()     # any page may be anywhere in the pools
+        self.ctx_len = torch.zeros(batch, dtype=torch.int32, device="cuda")
+        self.cache = koala.PagedCache(pools["k"], pools["v"], pools["k_scale"], pools["v_scale"], order.view(batch, pages), self.ctx_len)
+        self.capacity = pages * page
+        self.cos, self.sin = koala.rope_tables(self.capacity, dh, cfg["rope_base"])
+
+    def buffers(self, rows):
+        """What a verification of `rows` rows a sequence works in, for as long as a caller keeps it (and a graph over it)."""
+        B, c = self.batch, self.cfg
+        n, H, F, V, heads, dh = B * rows, c["hidden"], c["ffn"], c["vocab"], c["n_heads"], c["head_dim"]
+        new = lambda *s, dt=BF16: torch.empty(*s, dtype=dt, device="cuda")
+        return dict(tokens=new(B, rows, dt=torch.int32).zero_(), embedded=new(n, H), x=new(n, H, dt=F32), q8=new(n, -(-max(H, F) // 16) * 16, dt=torch.int8),
+                    scale=new(n, dt=F32), qkv=new(B, rows, 3 * heads, dh), q=new(B, rows, heads, dh), att=new(B, rows, heads, dh),
+                    gate_up=new(n, 2 * F), logits=new(n, V, dt=F32), feat=new(n, H, dt=F32), greedy=new(B, rows, dt=torch.int32))
+
+    def verify(self, b, depth=None, mask=None):
+        """Features, logits and greedy tokens of b["tokens"]'s rows behind the context; their keys and values go to the slots behind it."""
+        c, eps = self.cfg, self.cfg["rms_eps"]
+        n, H, F, heads = b["x"].shape[0], c["hidden"], c["ffn"], c["n_heads"]
+        x, q8, s = b["x"], b["q8"], b["scale"]
+        torch.index_select(self.embed, 0, b["tokens"].view(-1), out=b["embedded"])
+        x.copy_(b["embedded"])
+        for l, w in enumerate(self.layers):
+            koala.quantize_rows(x, q8[:, :H], s, form="norm", gain=w["in_norm"], eps=eps)
+            w["qkv"].forward(q8, s, b["qkv"].view(n, 3 * H))
+            q, k, v = b["qkv"].split(heads, 2)
+            self.cache.append(l, q, k, v, b["q"], self.cos, self.sin, depth=depth)
+            self.cache.attend(l, b["q"], b["att"], mask=mask, max_len=self.capacity)
+            koala.quantize_rows(b["att"].view(n, H), q8[:, :H], s)
+            w["o"].forward(q8, s, x, add=x)
+            koala.quantize_rows(x, q8[:, :H], s, form="norm", gain=w["post_norm"], eps=eps)
+            w["gate_up"].forward(q8, s, b["gate_up"])
+            koala.quantize_rows(b["gate_up"], q8[:, :F], s, form="swiglu")
+            w["down"].forward(q8, s, x, add=x)
+        koala.quantize_rows(x, q8[:, :H], s, form="norm", gain=self.final_norm, eps=eps)
+        self.head.forward(q8, s, b["logits"])
+        torch.mul(x * torch.rsqrt(x.square().mean(1, keepdim=True) + eps), self.final_norm.float(), out=b["feat"])
+        b["greedy"].copy_(b["logits"].argmax(1).view(self.batch, -1))
+        return b
+
+    def captured(self, b, depth=None, mask=None):
+        """verify over b as a graph: call the result after filling b["tokens"]."""
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            self.verify(b, depth, mask)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            self.verify(b, depth, mask)
+        return graph.replay
+
+    def prefill(self, prompt):
+        """Runs the prompt [batch, n] in pieces of up to `rows`; returns every position's features and the last one's greedy token."""
+        feats = []
+        for i in range(0, prompt.shape[1], self.rows):
+            piece = prompt[:, i:i + self.rows]
+            b = self.buffers(piece.shape[1])
+            b["tokens"].copy_(piece)
+            self.verify(b)
+            self.ctx_len += piece.shape[1]
+            feats.append(b["feat"].view(self.batch, piece.shape[1], -1))
+        return torch.cat(feats, 1), b["greedy"][:, -1]
+
+
+def generate(cfg, target, draft, prompt, new_tokens, capacity=512):
+    """Greedy generation of one sequence: an EAGLE-style head drafts, the quantised target verifies.  Returns the tokens and the
+    accepted length of every iteration."""
+    tree = cfg["tree_template"]
+    T, D, H = tree.n_nodes, tree.depth, cfg["hidden"]
+    weight = lambda n: koala.packing._dev(target, n, "cuda", "bf16")
+    model = QuantizedTarget(cfg, weight, 1, capacity)
+    # the draft head's context: its caches, and the lengths, which are the paged cache's own
+    shape = {k: cfg[k] for k in ("hidden", "n_heads", "head_dim", "ffn", "vocab", "n_layers", "rms_eps", "rope_base")}
+    ctx = koala.KoalaContext(dict(shape, dtype=koala.KOALA_BF16), dict(kind=koala.KOALA_DRAFT_EAGLE, K=cfg["K"], max_m=64), tree, 1)
+    weights = koala.pack_target_weights(target, cfg)
+    weights.update(koala.pack_eagle_weights(draft, cfg))
+    kv = koala.alloc_kv(cfg, 1, model.capacity, "cuda", cfg["K"])
+    kv["ctx_len"] = model.ctx_len
+    ctx.bind(weights, kv, torch.empty(ctx.workspace_bytes(), dtype=torch.uint8, device="cuda"))
+
+    feats, root = model.prefill(prompt.view(1, -1))
+    m = min(prompt.numel(), 64)
+    feat_in, tok_in = feats[:, -m:].contiguous(), torch.cat((prompt[-m + 1:] if m > 1 else prompt[:0], root.int())).view(1, -1).contiguous()
+    depth = [0]
+    for p in tree.parent[1:]:
+        depth.append(depth[int(p)] + 1)
+    b = model.buffers(T)
+    verify = model.captured(b, torch.tensor(depth, dtype=torch.int32, device="cuda"), koala.tree_masks(tree))
+    i32 = lambda *s: torch.empty(*s, dtype=torch.int32, device="cuda")
+    accept_len, path, nxt = i32(1), i32(1, D + 1), i32(1)
+    out, accepted = [int(root)], []
+    while len(out) < new_tokens:
+        ctx.draft_expand(1, feat_in, tok_in, tok_in.shape[1], b["tokens"])
+        verify()
+        ctx.accept_prefix(1, b["tokens"], b["greedy"], accept_len, path, nxt, commit=False)
+        model.cache.commit(accept_len, path)
+        a = int(accept_len)
+        nodes = path[0, :a + 1].long()
+        feat_in = b["feat"][nodes].view(1, a + 1, H)
+        tok_in = torch.cat((b["tokens"][0, nodes[1:]], nxt)).view(1, -1)
+        out += tok_in[0].tolist()
+        accepted.append(a)
+    ctx.close()
+    return out[:new_tokens], accepted
+
+
+def _time(tree, context):
+    """us of a verification at the 7B shape, quantised and 16-bit, random weights (four layers, as the others are like them)."""
+    cfg = dict(get_config("cfg2"), n_layers=4)
+    H, F, V, dh = cfg["hidden"], cfg["ffn"], cfg["vocab"], cfg["head_dim"]
+    sizes = dict(wq=(H, H), wk=(H, H), wv=(H, H), wo=(H, H), wgate=(F, H), wup=(F, H), wdown=(H, F), embed=(V, H), lm_head=(V, H))
+    weight = lambda n: torch.randn(sizes[n.split(".")[-1]], device="cuda", dtype=BF16) * 0.02 if n.split(".")[-1] in sizes else torch.ones(H, device="cuda", dtype=BF16)
+    model = QuantizedTarget(cfg, weight, 1, context + 64)
+    for p in model.cache._keep[:2]:
+        p.random_(0, 256)
+    for p in model.cache._keep[2:4]:
+        p.random_(124, 128)
+    model.ctx_len.fill_(context)
+    depth = [0]
+    for p in tree.parent[1:]:
+        depth.append(depth[int(p)] + 1)
+    b = model.buffers(tree.n_nodes)
+    replay = model.captured(b, torch.tensor(depth, dtype=torch.int32, device="cuda"), koala.tree_masks(tree))
+
+    shape = {k: cfg[k] for k in ("hidden", "n_heads", "head_dim", "ffn", "vocab", "n_layers", "rms_eps", "rope_base")}
+    ctx = koala.KoalaContext(dict(shape, dtype=koala.KOALA_BF16), dict(kind=koala.KOALA_DRAFT_MEDUSA, K=1, medusa_heads=tree.depth, max_m=1), tree, 1)
+    mat = koala.device_matrix
+    pair = koala.packing.rotary_pair_interleave
+    layer = lambda: (weight("n"), mat(torch.cat((pair(weight("wq"), dh), pair(weight("wk"), dh), weight("wv")))), mat(weight("wo")), weight("n"),
+                     mat(torch.cat((weight("wgate"), weight("wup")))), mat(weight("wdown")))
+    kv = koala.alloc_kv(cfg, 1, context + 128, "cuda")
+    kv["ctx_len"].fill_(context)
+    ctx.bind(dict(embed=weight("embed"), lm_head=mat(weight("lm_head")), final_norm=weight("n"), layers=[layer() for _ in range(4)], fc=None,
+                  draft=[mat(weight("wq")) for _ in range(tree.depth)]), kv, torch.empty(ctx.workspace_bytes(), dtype=torch.uint8, device="cuda"))
+    feat, greedy = torch.empty(1, tree.n_nodes, H, device="cuda"), torch.empty(1, tree.n_nodes, dtype=torch.int32, device="cuda")
+
+    def us(f, n=50):
+        for _ in range(5):
+            f()
+        a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(n):
+            f()
+        z.record()
+        torch.cuda.synchronize()
+        return a.elapsed_time(z) / n * 1e3
+    times = us(replay), us(lambda: ctx.tree_verify(1, b["tokens"], feat, None, greedy))
+    ctx.close()
+    return times
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--time", action="store_true")
+    a = ap.parse_args()
+    if a.time:
+        for context in (1024, 8192, 30000):
+            tree = get_config("cfg2")["tree_template"]
+            q, h = _time(tree, context)
+            print(f"7B shape, 4 layers and LM head, {tree.n_nodes} nodes, {context} keys: {q:.0f} us quantised, {h:.0f} us in 16 bits")
+        return
+    cfg = get_config("cfg2_small")
+    target, draft = predictable_pair(cfg, 0, sigma=6.0, cache=True)
+    tokens, accepted = generate(cfg, target, draft, torch.arange(200, 300, dtype=torch.int32, device="cuda"), 40)
+    print("generated:", tokens)
+    print(f"{len(accepted)} iterations, {sum(n + 1 for n in accepted) / len(accepted):.2f} tokens each")
+
+
+if __name__ == "__main__":
+    main()
