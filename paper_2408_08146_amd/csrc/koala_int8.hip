@@ -1,5 +1,6 @@
 // Projections in 8-bit integers with a scale for each token and each output channel (koala.h, "Projections in 8-bit integers").
 #include "koala_internal.h"
+#include <algorithm>
 #include <cmath>
 
 namespace {
@@ -219,17 +220,23 @@ struct LinearArgs {
     int *part;     // [splits][rows][out rounded up to 4] where splits > 1
 };
 
-// the four consecutive outputs n .. n + 3 of row m from their sums
-__device__ __forceinline__ void finish4(const LinearArgs &a, int m, int n, i32x4 s) {
-    if (m >= a.rows || n >= a.out) return;
-    const float qs = a.q_scale[m];
-    const size_t at = (size_t)m * a.ldy + n;
+// the scales of the channels n .. n + 3 (past the last, that one's)
+__device__ __forceinline__ f32x4 scales4(const LinearArgs &a, int n) {
     typedef float __attribute__((ext_vector_type(4), aligned(4))) f32x4_a4;
-    if (a.vec && n + 4 <= a.out) {
-        const f32x4 ws = *(const f32x4_a4 *)(a.w_scale + n);
-        f32x4 v;
+    if (n + 4 <= a.out) return *(const f32x4_a4 *)(a.w_scale + n);
+    f32x4 ws;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * qs * ws[e];
+    for (int e = 0; e < 4; ++e) ws[e] = a.w_scale[min(n + e, a.out - 1)];
+    return ws;
+}
+// the four consecutive outputs n .. n + 3 of row m from their sums and scales
+__device__ __forceinline__ void finish4(const LinearArgs &a, int m, int n, i32x4 s, float qs, f32x4 ws) {
+    if (m >= a.rows || n >= a.out) return;
+    const size_t at = (size_t)m * a.ldy + n;
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * qs * ws[e];
+    if (a.vec && n + 4 <= a.out) {
         if (a.y_f32) {
             if (a.add) v += *(const f32x4 *)((const float *)a.add + at);
             *(f32x4 *)((float *)a.y + at) = v;
@@ -245,10 +252,32 @@ __device__ __forceinline__ void finish4(const LinearArgs &a, int m, int n, i32x4
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if (n + e >= a.out) continue;
-        const float v = (float)s[e] * qs * a.w_scale[n + e];
-        if (a.y_f32) ((float *)a.y)[at + e] = v + (a.add ? ((const float *)a.add)[at + e] : 0.f);
-        else ((bf16_t *)a.y)[at + e] = (bf16_t)__builtin_bit_cast(uint16_t, (__bf16)(v + (a.add ? bf_lo(((const bf16_t *)a.add)[at + e]) : 0.f)));
+        if (a.y_f32) ((float *)a.y)[at + e] = v[e] + (a.add ? ((const float *)a.add)[at + e] : 0.f);
+        else ((bf16_t *)a.y)[at + e] = (bf16_t)__builtin_bit_cast(uint16_t, (__bf16)(v[e] + (a.add ? bf_lo(((const bf16_t *)a.add)[at + e]) : 0.f)));
     }
+}
+// a wave's tile: the rows m, m + 16, ... and the channels n .. n + 3, n + 16 .. n + 19, ... of a lane.  All scales are asked for at once: asked
+// for where they are used, behind stores that may change them for all the compiler knows, each would take memory's latency anew
+template <int TM, int TN> __device__ __forceinline__ void finish_tile(const LinearArgs &a, int split, int m, int n, i32x4 (&acc)[TN][TM]) {
+    if (a.splits > 1) {
+        const int ld = (a.out + 3) / 4 * 4;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                if (m + 16 * i < a.rows && n + 16 * j < a.out) *(i32x4 *)(a.part + ((size_t)split * a.rows + m + 16 * i) * ld + n + 16 * j) = acc[j][i];
+        return;
+    }
+    float qs[TM];
+    f32x4 ws[TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) qs[i] = a.q_scale[min(m + 16 * i, a.rows - 1)];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) ws[j] = scales4(a, n + 16 * j);
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int i = 0; i < TM; ++i) finish4(a, m + 16 * i, n + 16 * j, acc[j][i], qs[i], ws[j]);
 }
 
 // Up to 64 rows: the weights stream.  A workgroup owns U groups of 16 output channels; its eight waves take chunks of KC terms in turn.  A
@@ -270,6 +299,21 @@ __global__ __launch_bounds__(512) void k_linear_rows(LinearArgs a) {
     const int lr = l / LPR, lp = l % LPR, ldw = (int)a.ldw, ldq = (int)a.ldq;
     const rsrc_t wr = rows_from(a.w, a.ldw, n0, a.out, a.in), xr = rows_from(a.q, a.ldq, m0, a.rows, a.in);
     const unsigned w_lane = lr * ldw + 16 * lp, x_lane = lr * ldq + 16 * lp;
+    // a wave's part of the outputs, and their scales: asked for first, for nobody to wait for at the end
+    constexpr int PARTS = (U * MT + NW - 1) / NW;
+    auto part_row = [&](int p) { return m0 + 16 * (p % MT) + li; };
+    auto part_channel = [&](int p) { return n0 + 16 * (p / MT) + 4 * lg; };
+    float qs[PARTS];
+    f32x4 ws[PARTS];
+    auto scales = [&]() {
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            const int p = min(wave + NW * i, U * MT - 1);
+            qs[i] = a.q_scale[min(part_row(p), a.rows - 1)];
+            ws[i] = scales4(a, part_channel(p));
+        }
+    };
+    if (PARTS <= 2) scales();
     i32x4 acc[U][MT];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -313,34 +357,38 @@ __global__ __launch_bounds__(512) void k_linear_rows(LinearArgs a) {
                         acc[v < MT ? 0 : v - MT][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o, x[s][m], acc[v < MT ? 0 : v - MT][m], 0, 0, 0);
             }
         }
+    if (PARTS > 2) scales();   // no registers for them before
     __syncthreads();
-    // the waves' sums, the upper four onto the lower four, then these
+    // the waves' sums, the upper half onto the lower, then these
 #pragma unroll
     for (int half = 1; half >= 0; --half) {
-        if ((wave >> 2) == half)
+        if (wave / (NW / 2) == half)
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     if (half == 0) acc[u][m] += red[wave][u * MT + m][l];
-                    red[wave & 3][u * MT + m][l] = acc[u][m];
+                    red[wave % (NW / 2)][u * MT + m][l] = acc[u][m];
                 }
         __syncthreads();
     }
-    for (int p = wave; p < U * MT; p += NW) {
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        const int p = wave + NW * i;
+        if (p >= U * MT) break;
         i32x4 s = red[0][p][l];
 #pragma unroll
         for (int v = 1; v < NW / 2; ++v) s += red[v][p][l];
-        finish4(a, m0 + 16 * (p % MT) + li, n0 + 16 * (p / MT) + 4 * lg, s);
+        finish4(a, part_row(p), part_channel(p), s, qs[i], ws[i]);
     }
 }
 
-// More rows: tiles of BM rows by BN channels through LDS, WM x WN waves of 16 TM rows by 16 TN channels each; 128 terms at a time, the next
-// ones on their way into registers while these are multiplied.  A row's 16-byte pieces are stored at their place XOR the row's number
-// modulo 8: a wave's reads of 16 rows then meet different banks.
-template <int TM, int TN, int WM, int WN, int AHEAD>
-__global__ __launch_bounds__(64 * WM * WN) void k_linear_tiles(LinearArgs a) {
-    constexpr int NT = 64 * WM * WN, RPT = NT / 8, BM = 16 * TM * WM, BN = 16 * TN * WN, LX = BM / RPT, LW = BN / RPT;   // 16-byte loads a thread
+// More rows: tiles of 128 rows by 128 channels through LDS, four waves of 64 by 64; 128 terms at a time, three steps ahead on their way into
+// registers while one is multiplied, two workgroups a compute unit.  A row's 16-byte pieces are stored at their place XOR the row's number
+// modulo 8: a wave's reads then meet different banks.  480 x 35840 x 6656: 167 us, 1.37 POP/s; what bounds it is the wait for LDS and the
+// other waves in every step.
+__global__ __launch_bounds__(256) void k_linear_tiles(LinearArgs a) {
+    constexpr int TM = 4, TN = 4, WM = 2, WN = 2, AHEAD = 3, NT = 64 * WM * WN, RPT = NT / 8, BM = 16 * TM * WM, BN = 16 * TN * WN, LX = BM / RPT, LW = BN / RPT;   // 16-byte loads a thread
     __shared__ __attribute__((aligned(16))) int8_t sx[2][BM * 128], sw[2][BN * 128];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
     const int nm = (a.rows + BM - 1) / BM, nn = (a.out + BN - 1) / BN, total = nm * nn * a.splits;
@@ -405,15 +453,103 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_tiles(LinearArgs a) {
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             }
         }
-    const int ldp = (a.out + 3) / 4 * 4;
+    finish_tile<TM, TN>(a, sp, m0 + wm + li, n0 + wn + 4 * lg, acc);
+}
+
+// The largest products: tiles of 256 x 256, eight waves of 128 rows by 64 channels, 64 terms at a time.  Memory writes a step's operands
+// straight into LDS, four steps of 32 KB in turn: while one is multiplied, the next one is read into registers, the one after it has landed or
+// is landing and the two behind that are asked for.  The copies are placed by hand (the compiler would wait for all of them before any read
+// of LDS): a wave waits until all but the two newest steps of its own have landed, then all waves meet; that one barrier a step also says that
+// nobody reads the step that is written next any more.  LDS serves a wave's 16-byte reads in groups of 16 lanes, 0-3, 12-15, 20-23 and 24-27
+// first: with a piece at its place XOR `turned` of four rows' number, a group meets 16 different places of its 256 bytes (no conflicts counted).
+// Tiles are taken in bands of eight rows of tiles, so that the 32 that run on a die share their operands in its cache.
+// 2000 x 22016 x 4096: 191 us, 1.89 POP/s; 8192 x 8192 x 8192: 463 us, 2.38 POP/s (the library's product: 526).  There the matrix pipe is
+// busy for 59% of the cycles, and what bounds it is power: with the conflicts gone it took a tenth fewer cycles at a clock a tenth lower, 1.7 GHz.
+__device__ __forceinline__ void copy_to_lds(i32x4 rsrc, unsigned from, unsigned to) {   // 64 x 16 bytes, to `to` on in lanes' order
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(from), "s"(rsrc) : "memory");
+}
+__device__ __forceinline__ i32x4 raw_rows(const int8_t *p, size_t ld, int row, int rows, int cols) {
+    const uint64_t at = (uint64_t)(uintptr_t)(p + (size_t)row * ld);
+    const size_t left = (size_t)(rows - 1 - row) * ld + cols;
+    return (i32x4){(int)(uint32_t)at, (int)(uint32_t)(at >> 32) & 0xFFFF, left > 0x7FFFFF00ull ? 0x7FFFFF00 : (int)left, 0x00020000};
+}
+__device__ __forceinline__ int turned(int j) { return (0x78 >> 2 * j) & 3; }   // 0, 2, 3, 1
+__global__ __launch_bounds__(512) void k_linear_wide(LinearArgs a) {
+    constexpr int TM = 8, TN = 4, WM = 2, WN = 4, NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, STAGE = (BM + BN) * 64, STAGES = 4, CX = BM / 16 / NW, CW = BN / 16 / NW;
+    __shared__ __attribute__((aligned(1024))) int8_t lds[STAGES * STAGE];   // a stage: BM rows of 64 bytes, BN channels
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
+    const int nm = (a.rows + BM - 1) / BM, nn = (a.out + BN - 1) / BN, total = nm * nn * a.splits;
+    int t = (int)blockIdx.x;
+    const int per = total >> 3;
+    if (t < per * 8) t = (t & 7) * per + (t >> 3);
+    const int sp = t / (nm * nn);
+    t %= nm * nn;
+    // bands of eight tiles of rows
+    const int band = t / (8 * nn), bh = min(8, nm - 8 * band);
+    t -= band * 8 * nn;
+    const int m0 = (8 * band + t % bh) * BM, n0 = t / bh * BN;
+    const int chunks = (a.in + 63) / 64, c0 = (int)((long)chunks * sp / a.splits), c1 = (int)((long)chunks * (sp + 1) / a.splits);
+    const i32x4 xr = raw_rows(a.q, a.ldq, m0, a.rows, a.in), wr = raw_rows(a.w, a.ldw, n0, a.out, a.in);
+    unsigned o[CX + CW];
+#pragma unroll
+    for (int i = 0; i < CX + CW; ++i) {
+        const unsigned piece = ((l & 3) ^ turned(l >> 4)) * 16;
+        if (i < CX) o[i] = (unsigned)min((wave * CX + i) * 16 + (l >> 2), a.rows - 1 - m0) * (unsigned)a.ldq + piece;
+        else o[i] = (unsigned)min((wave * CW + i - CX) * 16 + (l >> 2), a.out - 1 - n0) * (unsigned)a.ldw + piece;
+    }
+    typedef __attribute__((address_space(3))) int8_t lds_byte;
+    const unsigned base = (unsigned)(uintptr_t)(lds_byte *)lds;
+    auto copy = [&](int c, int i) {
+        const unsigned k = min(c, c1 - 1) * 64, to = base + (c & (STAGES - 1)) * STAGE;
+        if (i < CX) copy_to_lds(xr, o[i] + k, to + (wave * CX + i) * 1024);
+        else copy_to_lds(wr, o[i] + k, to + BM * 64 + (wave * CW + i - CX) * 1024);
+    };
+    i32x4 acc[TN][TM];
 #pragma unroll
     for (int n = 0; n < TN; ++n)
 #pragma unroll
-        for (int m = 0; m < TM; ++m) {
-            const int row_ = m0 + wm + 16 * m + li, col = n0 + wn + 16 * n + 4 * lg;
-            if (a.splits == 1) finish4(a, row_, col, acc[n][m]);
-            else if (row_ < a.rows && col < a.out) *(i32x4 *)(a.part + ((size_t)sp * a.rows + row_) * ldp + col) = acc[n][m];
+        for (int m = 0; m < TM; ++m) acc[n][m] = (i32x4){0, 0, 0, 0};
+    const int wm = (wave % WM) * 16 * TM, wn = (wave / WM) * 16 * TN;
+    const int at = li * 64 + ((lg ^ turned(li >> 2)) << 4);
+    auto meet = [&]() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * (CX + CW)) : "memory"); };
+    i32x4 x[2][TM], w[2][TN];
+    auto read_x = [&](int c, int m) { return *(const i32x4 *)(lds + (c & (STAGES - 1)) * STAGE + (wm + 16 * m) * 64 + at); };
+    auto read_w = [&](int c, int n) { return *(const i32x4 *)(lds + (c & (STAGES - 1)) * STAGE + BM * 64 + (wn + 16 * n) * 64 + at); };
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int i = 0; i < CX + CW; ++i) copy(c0 + p, i);
+    meet();
+#pragma unroll
+    for (int m = 0; m < TM; ++m) x[0][m] = read_x(c0, m);
+#pragma unroll
+    for (int n = 0; n < TN; ++n) w[0][n] = read_w(c0, n);
+#pragma unroll
+    for (int i = 0; i < CX + CW; ++i) copy(c0 + 3, i);
+    const int lim = min(a.in, c1 * 64);
+    for (int c = c0; c < c1; c += 2)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int cc = c + u;
+            meet();
+            if (cc * 64 + 64 > lim) {   // terms past the end: whatever was copied, times zero
+                const bool in = cc * 64 + 16 * lg < lim;
+#pragma unroll
+                for (int m = 0; m < TM; ++m) x[u][m] = in ? x[u][m] : (i32x4){0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int n = 0; n < TN; ++n) {
+#pragma unroll
+                for (int i = n * (CX + CW) / TN; i < (n + 1) * (CX + CW) / TN; ++i) copy(cc + 4, i);
+#pragma unroll
+                for (int m = n * TM / TN; m < (n + 1) * TM / TN; ++m) x[u ^ 1][m] = read_x(cc + 1, m);
+                w[u ^ 1][n] = read_w(cc + 1, n);
+#pragma unroll
+                for (int m = 0; m < TM; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][n], x[u][m], acc[n][m], 0, 0, 0);
+            }
         }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // nothing is on its way into LDS when the workgroup ends
+    finish_tile<TM, TN>(a, sp, m0 + wm + li, n0 + wn + 4 * lg, acc);
 }
 
 // Sums of the splits, and the outputs: four a thread
@@ -424,7 +560,7 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
     const i32x4 *p = (const i32x4 *)a.part + (size_t)row * quads + quad;
     i32x4 s = p[0];
     for (int i = 1; i < a.splits; ++i) s += p[i * stride];
-    finish4(a, row, 4 * quad, s);
+    finish4(a, row, 4 * quad, s, a.q_scale[row], scales4(a, 4 * quad));
 }
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
@@ -446,10 +582,11 @@ struct Plan {
 };
 // The launch that takes the least time by what each form takes on 256 compute units (us, measured at 4096 to 17920 terms):
 // Row groups, up to 64 rows: a round of compute units takes as long as a workgroup's channels, and as one group more for its beginning
-// and end.  26 x 22016 x 4096 with 1, 2, 3, 4, 6, 8 groups: 26.1, 24.0, 23.0, 25.9, 23.5, 23.9; 60 x 12288: 23.7, 21.1, 16.5, 17.1, 22.6, 27.2.
-// Tiles: a compute unit takes 0.72 a chunk of 128 terms of a tile of 128 x 128 (two of which run side by side) and 2.0 of one of 256 x 256, and
-// 1.5 and 6 for a tile's beginning and end; splitting the terms costs a second launch and the partial sums' way there and back.
-// 2000 x 22016 x 4096: 274 (128), 222 (256); 480 x 35840 x 6656: 170, 214; 480 x 6656 x 17920 with 1, 2, 4 splits: 105, 95, 105 and 249, 137, 88.
+// and end.  26 x 22016 x 4096 with 1, 2, 3, 4, 6, 8 groups: 26.1, 24.0, 23.0, 25.9, 20.4, 20.3; 60 x 12288: 23.7, 21.1, 15.8, 17.1, 22.6, 27.2.
+// Tiles: of 128 x 128 a compute unit works on two at a time and takes 0.70 a chunk of 128 terms of each; of 256 x 256 on one, which takes 1.45
+// a chunk and 14 for its beginning and end.  Splitting the terms costs a second launch and the partial sums' way there and back.
+// 2000 x 22016 x 4096: 271 (128), 194 (256); 480 x 35840 x 6656: 167, 182; 2000 x 4096 x 4096: 46, 52; 480 x 6656 x 17920 with 1, 2, 3, 4, 6
+// splits: 105, 98, 103, 105, 106 and 203, 118, 95, 81, 115; 128 x 4096 x 4096: 28.5, 19.5, 16.5, 16.0, 15.2 and 49, 29, 24, 22, 21.
 Plan plan_of(int rows, int out, int in) {
     Plan p{Plan::ROWS, 1, 1};
     if (rows <= 64) {
@@ -472,8 +609,9 @@ Plan plan_of(int rows, int out, int in) {
         const double tiles = (double)((rows + side - 1) / side) * ((out + side - 1) / side);
         if (tiles * 16 > 2147483647.0) continue;
         for (int s = 1; s <= 16 && s <= chunks; ++s) {
-            const double each = (chunks + s - 1) / s * (f == Plan::TILE128 ? 0.72 : 2.0) + (f == Plan::TILE128 ? 1.5 : 6.0);
-            const double us = std::ceil(tiles * s / 256) * each + (s > 1 ? 4.0 + (double)s * rows * out * 8 / 1e7 : 0.0);
+            const double chunk = (chunks + s - 1) / s, rounds = tiles * s / 256;
+            const double us = (f == Plan::TILE128 ? std::max(rounds, 1.0) * chunk * 0.70 + 8.0 : std::ceil(rounds) * (chunk * 1.45 + 14.0)) +
+                              (s > 1 ? 4.0 + (double)s * rows * out * 8 / 1e7 : 0.0);
             if (us < best) {
                 best = us;
                 p.form = f;
@@ -497,10 +635,6 @@ template <int MT> void rows_by_units(hipStream_t st, const LinearArgs &a, int un
     default: if constexpr (MT < 4) rows_launch<8, MT, MT == 1 ? 3 : 5>(st, a); break;
     }
 }
-template <int TM, int TN, int WM, int WN, int AHEAD> void tiles_launch(hipStream_t st, const LinearArgs &a) {
-    constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN;
-    k_linear_tiles<TM, TN, WM, WN, AHEAD><<<(a.rows + BM - 1) / BM * ((a.out + BN - 1) / BN) * a.splits, 64 * WM * WN, 0, st>>>(a);
-}
 void launch_linear(hipStream_t st, const LinearArgs &a, const Plan &p) {
     if (p.form == Plan::ROWS) {
         if (a.rows <= 16) rows_by_units<1>(st, a, p.units);
@@ -508,8 +642,8 @@ void launch_linear(hipStream_t st, const LinearArgs &a, const Plan &p) {
         else rows_by_units<4>(st, a, p.units);
         return;
     }
-    if (p.form == Plan::TILE128) tiles_launch<4, 4, 2, 2, 3>(st, a);
-    else tiles_launch<8, 4, 2, 4, 2>(st, a);
+    if (p.form == Plan::TILE128) k_linear_tiles<<<(a.rows + 127) / 128 * ((a.out + 127) / 128) * a.splits, 256, 0, st>>>(a);
+    else k_linear_wide<<<(a.rows + 255) / 256 * ((a.out + 255) / 256) * a.splits, 512, 0, st>>>(a);
     if (a.splits > 1) k_linear_join<<<(unsigned)(((size_t)a.rows * ((a.out + 3) / 4) + 255) / 256), 256, 0, st>>>(a);
 }
 

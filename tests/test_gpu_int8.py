@@ -122,6 +122,26 @@ def test_products(f32, rows, out, cols):
     assert (wide[:, :3] == 5).all() and (wide[:, 3 + out:] == 5).all()
 
 
+@pytest.mark.parametrize("rows,out,cols", [(2047, 8001, 4144), (1999, 4095, 11056), (700, 6650, 12304), (1023, 3999, 9040), (2000, 8192, 1088)])
+def test_products_of_many_rows(rows, out, cols):
+    """Tiles of 256 by 256 in one, two, three or four parts of the sums, with an odd number of steps and ends inside of them; whatever
+    stands behind a row's end takes no part."""
+    import torch
+    rng = np.random.default_rng(rows)
+    q, w = (rng.integers(-128, 128, (n, cols + 16), dtype=np.int8) for n in (rows, out))
+    q[:, :16] = w[:, :16] = -128
+    qs, ws = (np.exp(rng.standard_normal(n)).astype(np.float32) * 0.01 for n in (rows, out))
+    q, w = dev(q)[:, :cols], dev(w)[:, :cols]
+    want = ((q.double() @ w.double().T) * dev(qs).double()[:, None] * dev(ws).double()).cpu().numpy()   # the sums are exact
+    y = torch.full((rows, out), 7.0, device="cuda")
+    lin = QuantizedLinear(w, dev(ws))
+    lin.forward(q, dev(qs), y)
+    assert agrees(y, want, 4 * 2.0 ** -24 * np.abs(want), True)
+    z = torch.full((rows, out), 3.0, dtype=torch.bfloat16, device="cuda")
+    lin.forward(q, dev(qs), z, add=z)
+    assert agrees(z, want + 3.0, 4 * 2.0 ** -24 * (np.abs(want) + 3.0), False)
+
+
 def test_the_longest_sum_of_the_largest_products_fits():
     import torch
     q = torch.full((3, 131056), -128, dtype=torch.int8, device="cuda")
