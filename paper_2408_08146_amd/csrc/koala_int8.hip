@@ -18,10 +18,25 @@ __device__ __forceinline__ uint32_t bf_pair(float a, float b) {   // round to ne
 }
 __device__ __forceinline__ float bf_hi(uint32_t p) { return __uint_as_float(p & 0xFFFF0000u); }
 
+// Operands are read through buffer instructions: an address is one 32-bit offset a lane, and what lies outside the rows from `row` on
+// reads as zero.  (The whole offset is the lane's: the bounds check is of that one.)
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+constexpr unsigned OUTSIDE = 0x7FFFFFF0;   // an offset outside of any buffer, and whatever is added to it
+constexpr int STREAMED = 2;                // cache policy of what is read once
+__device__ __forceinline__ rsrc_t rows_from(const int8_t *p, size_t ld, int row, int rows, int cols) {
+    const size_t left = (size_t)(rows - 1 - row) * ld + cols;   // row < rows
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p + (size_t)row * ld), 0, left > 0x7FFFFF00ull ? 0x7FFFFF00 : (int)left, 0x00020000);
+}
+template <int AUX = 0> __device__ __forceinline__ i32x4 load16(rsrc_t r, unsigned lane, unsigned more) {
+    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(lane + more), 0, AUX));
+}
+
 // ---------------------------------------------------------------------------------------------
 // Rows to 8 bits.  A workgroup a row; a thread holds chunks of eight values (thread, thread + threads, ...) in registers, so the
-// row is read once for the sum of squares, the largest magnitude and the rounding.  Rows wider than CH chunks a thread (CH = 0) are
-// read again for each of them.
+// row is read once for the sum of squares, the largest magnitude and the rounding.  All of a thread's loads, the gain's too, are asked for
+// before the first is used and without a branch: what lies past a row's end reads as zero.  Rows wider than CH chunks a thread (CH = 0)
+// are read again for each of the three.  Bound by memory where rows are many: gated 2000 x 17920 fp32 62 us, 5.2 TB/s; 2000 x 11008 bfloat16
+// 23 us, 4.8 TB/s; by a launch and a row's way there and back where they are few: one row of 4096 2.7 us.
 // ---------------------------------------------------------------------------------------------
 struct QuantArgs {
     const void *x, *gain;
@@ -52,16 +67,60 @@ template <bool F32> __device__ __forceinline__ void load8(const void *src, size_
             x[e] = i + e >= n ? 0.f : F32 ? ((const float *)src)[row + i + e] : bf_lo(((const bf16_t *)src)[row + i + e]);
     }
 }
-
-__device__ __forceinline__ float wave_sum(float x) {
+// the same as they lie in memory, from a row of n of them (at most 2^17) that `rsrc` describes
+template <bool F32> struct Eight {
+    i32x4 w[F32 ? 2 : 1];
+    __device__ __forceinline__ void values(float *x) const {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    return x;
+        for (int e = 0; e < 4; ++e)
+            if (F32) {
+                x[e] = __int_as_float(w[0][e]);
+                x[4 + e] = __int_as_float(w[F32 ? 1 : 0][e]);
+            } else {
+                x[2 * e] = bf_lo((uint32_t)w[0][e]);
+                x[2 * e + 1] = bf_hi((uint32_t)w[0][e]);
+            }
+    }
+};
+template <bool F32> __device__ __forceinline__ rsrc_t row_of(const void *src, size_t row, int n) {   // an odd last bfloat16 is not part of it
+    return __builtin_amdgcn_make_buffer_rsrc(F32 ? (void *)((float *)src + row) : (void *)((bf16_t *)src + row), 0, F32 ? 4 * n : 2 * n & ~3, 0x00020000);
 }
-__device__ __forceinline__ unsigned wave_max(unsigned x) {
+template <bool F32> __device__ __forceinline__ Eight<F32> eight_of(rsrc_t rsrc, const void *src, size_t row, int i, int n) {
+    Eight<F32> r;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x = max(x, (unsigned)__shfl_xor((int)x, o));
-    return x;
+    for (int z = 0; z < (F32 ? 2 : 1); ++z) r.w[z] = load16(rsrc, i * (F32 ? 4 : 2), 16 * z);
+    if (!F32 && (n & 1) && i == ((n - 1) & ~7)) {
+        const uint32_t last = ((const bf16_t *)src)[row + n - 1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e == (n - 1 - i) >> 1) r.w[0][e] = (int)last;
+    }
+    return r;
+}
+
+// over the 64 lanes of a wave, in all of them
+template <int CTRL> __device__ __forceinline__ uint32_t turned_row(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
+template <class F> __device__ __forceinline__ uint32_t over_row(uint32_t x, F f) {   // 16 lanes: each 8, 4, 2, 1 further on
+    x = f(x, turned_row<0x128>(x));
+    x = f(x, turned_row<0x124>(x));
+    x = f(x, turned_row<0x122>(x));
+    return f(x, turned_row<0x121>(x));
+}
+template <class F> __device__ __forceinline__ uint32_t over_wave(uint32_t x, F f) {
+    x = over_row(x, f);
+    const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = f(p[0], p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return f(q[0], q[1]);
+}
+// over a workgroup's waves, at most 16
+template <class F> __device__ __forceinline__ uint32_t over_workgroup(uint32_t x, uint32_t *lds, F f) {
+    x = over_wave(x, f);
+    const int tid = threadIdx.x, nw = blockDim.x >> 6;
+    if (nw == 1) return x;
+    if ((tid & 63) == 0) lds[tid >> 6] = x;
+    __syncthreads();
+    return over_row((tid & 15) < nw ? lds[tid & 15] : 0u, f);
 }
 
 // e^x to about two units in the last place: a power of two, and what its argument's rounding left out
@@ -73,38 +132,57 @@ __device__ __forceinline__ float exp_of(float x) {
 
 template <int FORM, bool F32, int CH>
 __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
-    __shared__ float s_sum[16];
-    __shared__ unsigned s_top[16];
-    const int tid = threadIdx.x, nt = blockDim.x, wave = tid >> 6, nw = nt >> 6, cols = a.cols;
+    __shared__ uint32_t s_sum[16], s_top[16];
+    const int tid = threadIdx.x, nt = blockDim.x, cols = a.cols;
     const size_t row = blockIdx.x, from = row * a.ldx;
     const int nch = (cols + 7) / 8;
-    constexpr int HELD = CH > 0 ? CH : 1;
-    float v[HELD][8];
-    // the chunk's values, the norm's row factor not yet applied
+    constexpr int HELD = CH > 0 ? CH : 1, PER = FORM == KOALA_ROWS_SWIGLU ? 2 : 1;   // PER: what is read for a value
+    float v[HELD][8], g[HELD][8];
+    auto gated = [](const float *p, float *x) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = p[2 * e] * __builtin_amdgcn_rcpf(1.f + exp_of(-p[2 * e])) * p[2 * e + 1];
+    };
+    // a chunk's values, the norm's row factor not yet applied
     auto take = [&](int c, float *x) {
         if (FORM == KOALA_ROWS_SWIGLU) {
             float p[16];
             load8<F32>(a.x, from, 16 * c, 2 * cols, p);
             load8<F32>(a.x, from, 16 * c + 8, 2 * cols, p + 8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = p[2 * e] * __builtin_amdgcn_rcpf(1.f + exp_of(-p[2 * e])) * p[2 * e + 1];
+            gated(p, x);
         } else {
             load8<F32>(a.x, from, 8 * c, cols, x);
         }
     };
-    auto gains = [&](int c, float *g) {
-        if (a.gain_f32) load8<true>(a.gain, 0, 8 * c, cols, g);
-        else load8<false>(a.gain, 0, 8 * c, cols, g);
-    };
-    if (CH > 0)
+    if (CH > 0) {
+        const rsrc_t xr = row_of<F32>(a.x, from, PER * cols);
+        Eight<F32> x[HELD][PER];
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+#pragma unroll
+            for (int z = 0; z < PER; ++z) x[i][z] = eight_of<F32>(xr, a.x, from, (PER * (tid + i * nt) + z) * 8, PER * cols);
+        if (FORM == KOALA_ROWS_NORM) {
+            if (a.gain_f32) {
+                const rsrc_t gr = row_of<true>(a.gain, 0, cols);
+#pragma unroll
+                for (int i = 0; i < HELD; ++i) eight_of<true>(gr, a.gain, 0, (tid + i * nt) * 8, cols).values(g[i]);
+            } else {
+                const rsrc_t gr = row_of<false>(a.gain, 0, cols);
+#pragma unroll
+                for (int i = 0; i < HELD; ++i) eight_of<false>(gr, a.gain, 0, (tid + i * nt) * 8, cols).values(g[i]);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
-            const int c = tid + i * nt;
-            if (c < nch) take(c, v[i]);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+            if (FORM == KOALA_ROWS_SWIGLU) {
+                float p[16];
+                x[i][0].values(p);
+                x[i][PER - 1].values(p + 8);
+                gated(p, v[i]);
+            } else {
+                x[i][0].values(v[i]);
+            }
         }
+    }
     float r = 1.f;
     if (FORM == KOALA_ROWS_NORM) {
         float sum = 0.f;
@@ -120,22 +198,23 @@ __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
                 take(c, v[0]);
                 add(v[0]);
             }
-        sum = wave_sum(sum);
-        if ((tid & 63) == 0) s_sum[wave] = sum;
-        __syncthreads();
-        sum = 0.f;
-        for (int w = 0; w < nw; ++w) sum += s_sum[w];
+        sum = __uint_as_float(over_workgroup(__float_as_uint(sum), s_sum, [](uint32_t x, uint32_t y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); }));
         r = 1.f / sqrtf(sum / (float)cols + a.eps);
     }
-    auto scaled = [&](int c, float *x) {
-        if (FORM != KOALA_ROWS_NORM) return;
-        float g[8];
-        gains(c, g);
+    auto scaled = [&](float *x, const float *g) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
     };
+    auto take_scaled = [&](int c, float *x) {
+        take(c, x);
+        if (FORM == KOALA_ROWS_NORM) {
+            if (a.gain_f32) load8<true>(a.gain, 0, 8 * c, cols, g[0]);
+            else load8<false>(a.gain, 0, 8 * c, cols, g[0]);
+            scaled(x, g[0]);
+        }
+    };
     // the largest magnitude by its bits: an infinity or not-a-number is larger than any number
-    unsigned top = 0;
+    uint32_t top = 0;
     auto look = [&](const float *x) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7FFFFFFFu);
@@ -143,37 +222,40 @@ __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
     if (CH > 0)
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
-            const int c = tid + i * nt;
-            if (c < nch) scaled(c, v[i]);
-            look(v[i]);
+            if (FORM == KOALA_ROWS_NORM) scaled(v[i], g[i]);
+            if (tid + i * nt < nch) look(v[i]);
         }
     else
         for (int c = tid; c < nch; c += nt) {
-            take(c, v[0]);
-            scaled(c, v[0]);
+            take_scaled(c, v[0]);
             look(v[0]);
         }
-    top = wave_max(top);
-    if ((tid & 63) == 0) s_top[wave] = top;
-    __syncthreads();
-    top = 0;
-    for (int w = 0; w < nw; ++w) top = max(top, s_top[w]);
+    top = over_workgroup(top, s_top, [](uint32_t x, uint32_t y) { return max(x, y); });
     const bool bad = top >= 0x7F800000u;
     float scale = __uint_as_float(top) / 127.f;
     if (!(scale > 0.f)) scale = 1.f;   // all zero (or so small that a scale would be): whole numbers are zero
     if (tid == 0) a.scale[row] = bad ? __builtin_nanf("") : scale;
     // x / scale by the scale's reciprocal and one step for what is left, which rounds as a division does, in a third of its instructions;
-    // scales whose reciprocal is near the ends of the range are divided by
+    // scales whose reciprocal is near the ends of the range are divided by.  Adding 3 2^22 leaves the nearest whole number in a sum's last bits.
     const float inv = 1.f / scale;
     const bool plain = scale > 0x1p-100f && scale < 0x1p100f;
     auto put = [&](int c, const float *x) {
-        uint32_t w[2] = {0, 0};
-        if (!bad)
+        uint32_t d[8], w[2];
+        if (plain) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float q = x[e] * inv, d = plain ? __builtin_fmaf(__builtin_fmaf(-q, scale, x[e]), inv, q) : x[e] / scale;
-                w[e >> 2] |= ((uint32_t)(int)rintf(d) & 0xFFu) << (8 * (e & 3));
+                const float q = x[e] * inv;
+                d[e] = __float_as_uint(__builtin_fmaf(__builtin_fmaf(-q, scale, x[e]), inv, q) + 0x1.8p23f);
             }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[e] = __float_as_uint(x[e] / scale + 0x1.8p23f);
+        }
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            const uint32_t lo = __builtin_amdgcn_perm(d[4 * z + 1], d[4 * z], 0x0C0C0400), hi = __builtin_amdgcn_perm(d[4 * z + 3], d[4 * z + 2], 0x04000C0C);
+            w[z] = bad ? 0u : lo | hi;
+        }
         *(u32x2 *)(a.q + row * a.ldq + 8 * c) = (u32x2){w[0], w[1]};
     };
     if (CH > 0)
@@ -184,24 +266,10 @@ __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
         }
     else
         for (int c = tid; c < nch; c += nt) {
-            take(c, v[0]);
-            scaled(c, v[0]);
+            take_scaled(c, v[0]);
             put(c, v[0]);
         }
     if (tid == 0 && (nch & 1)) *(u32x2 *)(a.q + row * a.ldq + 8 * nch) = (u32x2){0u, 0u};
-}
-
-// Operands are read through buffer instructions: an address is one 32-bit offset a lane, and what lies outside the rows from `row` on
-// reads as zero.  (The whole offset is the lane's: the bounds check is of that one.)
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
-constexpr unsigned OUTSIDE = 0x7FFFFFF0;   // an offset outside of any buffer, and whatever is added to it
-constexpr int STREAMED = 2;                // cache policy of what is read once
-__device__ __forceinline__ rsrc_t rows_from(const int8_t *p, size_t ld, int row, int rows, int cols) {
-    const size_t left = (size_t)(rows - 1 - row) * ld + cols;   // row < rows
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p + (size_t)row * ld), 0, left > 0x7FFFFF00ull ? 0x7FFFFF00 : (int)left, 0x00020000);
-}
-template <int AUX = 0> __device__ __forceinline__ i32x4 load16(rsrc_t r, unsigned lane, unsigned more) {
-    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(lane + more), 0, AUX));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -566,11 +634,14 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 koala_status launched() { return hipGetLastError() == hipSuccess ? KOALA_OK : KOALA_E_DEVICE; }
 
+// Two chunks a thread: loads enough under way, and as many rows at once as the chip holds.  2000 rows of 4096 bfloat16 with 1, 2, 4 and 8: 9.0,
+// 6.2, 6.5, 6.8 us; gated 2000 x 11008: 26.6, 23.0, 24.4, 25.6; normalised 26 x 4096 fp32: 3.3, 3.1, 3.5, 5.5.  Wider rows four, spread evenly:
+// gated 480 x 17920 11.3 (13.1 with 1024 threads, half of them with a third chunk).
 template <int FORM, bool F32> void quantize(hipStream_t st, const QuantArgs &a, int rows) {
-    const int nch = (a.cols + 7) / 8;
-    const int threads = nch >= 1024 ? 1024 : (nch + 63) / 64 * 64;
-    if (nch <= threads) k_quantize_rows<FORM, F32, 1><<<rows, threads, 0, st>>>(a);
-    else if (nch <= 2 * threads) k_quantize_rows<FORM, F32, 2><<<rows, threads, 0, st>>>(a);
+    const int nch = (a.cols + 7) / 8, held = nch <= 64 ? 1 : nch <= 2048 ? 2 : 4;
+    const int threads = std::min((((nch + held - 1) / held) + 63) / 64 * 64, 1024);
+    if (held == 1) k_quantize_rows<FORM, F32, 1><<<rows, threads, 0, st>>>(a);
+    else if (held == 2) k_quantize_rows<FORM, F32, 2><<<rows, threads, 0, st>>>(a);
     else if (nch <= 4 * threads) k_quantize_rows<FORM, F32, 4><<<rows, threads, 0, st>>>(a);
     else k_quantize_rows<FORM, F32, 0><<<rows, threads, 0, st>>>(a);
 }

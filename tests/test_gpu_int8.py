@@ -39,7 +39,7 @@ def quantized(x, form="plain", gain=None, eps=1e-6, bf16=False, pad=0, extra=0):
 
 
 @pytest.mark.parametrize("bf16", [True, False])
-@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 8), (3, 15), (2, 16), (65, 17), (3, 100), (26, 4096), (2, 8200), (1, 17920), (2, 33001), (3, 70016)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 8), (3, 15), (2, 16), (65, 17), (3, 100), (26, 4096), (2, 8200), (1, 17920), (2, 33001), (3, 70016), (3, 4099), (2, 20001)])
 def test_plain_rows_are_rounded_as_defined(bf16, rows, cols):
     rng = np.random.default_rng(cols)
     x = rounded(rng.standard_normal((rows, cols)) * np.exp(2 * rng.standard_normal((rows, 1))), bf16)
@@ -57,7 +57,7 @@ def silu(x):
 
 @pytest.mark.parametrize("bf16", [True, False])
 @pytest.mark.parametrize("form", ["norm", "swiglu"])
-@pytest.mark.parametrize("rows,cols", [(1, 7), (3, 64), (26, 4096), (2, 13824), (2, 40007)])
+@pytest.mark.parametrize("rows,cols", [(1, 7), (3, 64), (26, 4096), (2, 13824), (2, 40007), (3, 1001), (2, 20001)])
 def test_normed_and_gated_rows(bf16, form, rows, cols):
     """A value rounds to within half a step of the scale; the value itself and the scale are fp32: the sum of squares of n terms is
     within (n / 1024 + 20) 2^-24 (n terms over at least 64 threads, joined in a tree), everything else a few roundings."""
