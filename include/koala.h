@@ -441,8 +441,8 @@ koala_status koala_quantize_rows(void *hip_stream, int form, int x_dtype, int ro
 koala_status koala_linear_workspace_bytes(int rows, int out_features, int in_features, size_t *out);
 
 /* y[r][n] = q_scale[r] * w_scale[n] * sum_k q[r][k] w[n][k] (+ add[r][n]), rounded once where y is bfloat16.
- *   in_features a multiple of 16 and at most 131056 (the sum fits 32 bits for all int8 values); rows and out_features any; q_stride and
- *          w_stride at most 2^22;
+ *   in_features a multiple of 16 and at most 131056 (the sum fits 32 bits for all int8 values); rows and out_features at most
+ *          2^26, their product 2^37; q_stride and w_stride at most 2^22;
  *   add    device, the type and stride of y, may be NULL and may be y itself (a residual stream updated in place);
  *   y      device [rows, out_features] of y_dtype. */
 koala_status koala_linear_quantized(void *hip_stream, int rows, int out_features, int in_features, const int8_t *q,

@@ -646,6 +646,7 @@ template <int FORM, bool F32> void quantize(hipStream_t st, const QuantArgs &a, 
     else k_quantize_rows<FORM, F32, 0><<<rows, threads, 0, st>>>(a);
 }
 
+constexpr int LONGEST = 1 << 26;   // rows or output channels: they are counted in 32 bits, and so are workgroups of up to 2^37 outputs
 struct Plan {
     enum Form { ROWS, TILE128, TILE256 } form;
     int units;    // ROWS: groups of 16 channels a workgroup
@@ -678,8 +679,8 @@ Plan plan_of(int rows, int out, int in) {
     for (Plan::Form f : {Plan::TILE128, Plan::TILE256}) {
         const int side = f == Plan::TILE128 ? 128 : 256;
         const double tiles = (double)((rows + side - 1) / side) * ((out + side - 1) / side);
-        if (tiles * 16 > 2147483647.0) continue;
         for (int s = 1; s <= 16 && s <= chunks; ++s) {
+            if (s > 1 && (double)rows * out > (1 << 30)) break;   // (joined by outputs counted in 32 bits)
             const double chunk = (chunks + s - 1) / s, rounds = tiles * s / 256;
             const double us = (f == Plan::TILE128 ? std::max(rounds, 1.0) * chunk * 0.70 + 8.0 : std::ceil(rounds) * (chunk * 1.45 + 14.0)) +
                               (s > 1 ? 4.0 + (double)s * rows * out * 8 / 1e7 : 0.0);
@@ -731,7 +732,7 @@ koala_status koala_quantize_rows(void *hip_stream, int form, int x_dtype, int ro
     if (rows < 1 || cols < 1 || cols > (1 << 30) || x_stride < (form == KOALA_ROWS_SWIGLU ? 2ll * cols : cols) ||
         q_stride < (cols + 15) / 16 * 16 || (form == KOALA_ROWS_NORM && !(eps >= 0.f)))
         return KOALA_E_SHAPE;
-    if (!aligned16(x) || !aligned16(q) || ((uintptr_t)scale & 3) || (x_stride * (x_dtype == KOALA_FP32 ? 4 : 2)) % 16 || q_stride % 16 ||
+    if (!aligned16(x) || !aligned16(q) || ((uintptr_t)scale & 3) || x_stride % (x_dtype == KOALA_FP32 ? 4 : 8) || q_stride % 16 ||
         (form == KOALA_ROWS_NORM && !aligned16(gain)))
         return KOALA_E_ALIGN;
     QuantArgs a{x, gain, (size_t)x_stride, (size_t)q_stride, cols, eps, q, scale, gain_dtype == KOALA_FP32};
@@ -747,7 +748,9 @@ koala_status koala_quantize_rows(void *hip_stream, int form, int x_dtype, int ro
 
 koala_status koala_linear_workspace_bytes(int rows, int out_features, int in_features, size_t *out) {
     if (!out) return KOALA_E_NULL;
-    if (rows < 1 || out_features < 1 || in_features < 16 || in_features % 16 || in_features > 131056) return KOALA_E_SHAPE;
+    if (rows < 1 || out_features < 1 || in_features < 16 || in_features % 16 || in_features > 131056 || rows > LONGEST || out_features > LONGEST ||
+        (long)rows * out_features > 1l << 37)
+        return KOALA_E_SHAPE;
     const Plan p = plan_of(rows, out_features, in_features);
     *out = p.splits > 1 ? (size_t)p.splits * rows * ((out_features + 3) / 4) * 16 : 0;
     return KOALA_OK;

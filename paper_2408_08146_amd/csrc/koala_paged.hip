@@ -842,7 +842,7 @@ Pool pool_of(const koala_paged_kv *kv, int layer) {
 }
 koala_status launched() { return hipGetLastError() == hipSuccess ? KOALA_OK : KOALA_E_DEVICE; }
 // workgroups of 256 for n lanes; 0 if the lanes cannot be counted in 32 bits
-unsigned blocks_of(size_t n) { return n > 0xFFFFFF00ull ? 0 : (unsigned)((n + 255) / 256); }
+unsigned blocks_of(double n) { return n > 4294967040.0 ? 0 : (unsigned)(((size_t)n + 255) / 256); }
 
 int attend_wgs(int cu) { return 2 * cu; }
 int compute_units() {
@@ -899,7 +899,7 @@ koala_status koala_paged_append(const koala_paged_kv *kv, void *hip_stream, int 
     a.q = q; a.k = k; a.v = v;
     a.ldq = (size_t)q_stride; a.ldk = (size_t)k_stride; a.ldv = (size_t)v_stride;
     a.q_out = q_out;
-    const unsigned g = blocks_of((size_t)a.rows * (n_heads + 2 * KV) * (DH / 16));
+    const unsigned g = blocks_of((double)a.rows * (n_heads + 2 * KV) * (DH / 16));
     if (!g) return KOALA_E_SHAPE;
     hipStream_t st = (hipStream_t)hip_stream;
     if (DH == 128) {
@@ -923,7 +923,7 @@ koala_status koala_paged_read(const koala_paged_kv *kv, void *hip_stream, int la
     ReadArgs a{};
     a.p = pool_of(kv, layer);
     a.start = start; a.batch = (unsigned)batch; a.n = (unsigned)n; a.layers = (unsigned)n_layers; a.k_out = k_out; a.v_out = v_out;
-    const unsigned g = blocks_of((size_t)n_layers * batch * n * kv->n_kv_heads * (kv->head_dim / 8));
+    const unsigned g = blocks_of((double)n_layers * batch * n * kv->n_kv_heads * (kv->head_dim / 8));
     if (!g) return KOALA_E_SHAPE;
     hipStream_t st = (hipStream_t)hip_stream;
     if (kv->head_dim == 128) {
@@ -947,7 +947,7 @@ koala_status koala_paged_commit(const koala_paged_kv *kv, void *hip_stream, int 
     a.ctx_len = kv->ctx_len; a.accept_len = accept_len; a.accept_path = accept_path;
     a.path_stride = path_stride; a.batch = (unsigned)batch; a.layers = (unsigned)kv->n_layers;
     a.new_len = new_len == kv->ctx_len ? nullptr : new_len;
-    const unsigned g = blocks_of((size_t)kv->n_layers * batch * kv->n_kv_heads * (kv->head_dim / 16 + 2));
+    const unsigned g = blocks_of((double)kv->n_layers * batch * kv->n_kv_heads * (kv->head_dim / 16 + 2));
     if (!g) return KOALA_E_SHAPE;
     hipStream_t st = (hipStream_t)hip_stream;
     if (kv->head_dim == 128) k_paged_commit<128><<<g, 256, 0, st>>>(a);
