@@ -283,7 +283,7 @@ struct LinearArgs {
     const void *add;
     void *y;
     int rows, out, in;
-    bool y_f32, vec;   // vec: rows of y (and add) begin on four elements
+    bool y_f32;
     int splits;
     int *part;     // [splits][rows][out rounded up to 4] where splits > 1
 };
@@ -304,16 +304,18 @@ __device__ __forceinline__ void finish4(const LinearArgs &a, int m, int n, i32x4
     f32x4 v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * qs * ws[e];
-    if (a.vec && n + 4 <= a.out) {
+    if (n + 4 <= a.out) {   // (rows of y need not begin on more than an element)
+        typedef float __attribute__((ext_vector_type(4), aligned(4))) f32x4_any;
+        typedef unsigned int __attribute__((ext_vector_type(2), aligned(2))) u32x2_any;
         if (a.y_f32) {
-            if (a.add) v += *(const f32x4 *)((const float *)a.add + at);
-            *(f32x4 *)((float *)a.y + at) = v;
+            if (a.add) v += *(const f32x4_any *)((const float *)a.add + at);
+            *(f32x4_any *)((float *)a.y + at) = v;
         } else {
             if (a.add) {
-                const u32x2 d = *(const u32x2 *)((const bf16_t *)a.add + at);
+                const u32x2 d = *(const u32x2_any *)((const bf16_t *)a.add + at);
                 v += (f32x4){bf_lo(d[0]), bf_hi(d[0]), bf_lo(d[1]), bf_hi(d[1])};
             }
-            *(u32x2 *)((bf16_t *)a.y + at) = (u32x2){bf_pair(v[0], v[1]), bf_pair(v[2], v[3])};
+            *(u32x2_any *)((bf16_t *)a.y + at) = (u32x2){bf_pair(v[0], v[1]), bf_pair(v[2], v[3])};
         }
         return;
     }
@@ -524,10 +526,10 @@ __global__ __launch_bounds__(256) void k_linear_tiles(LinearArgs a) {
     finish_tile<TM, TN>(a, sp, m0 + wm + li, n0 + wn + 4 * lg, acc);
 }
 
-// The largest products: tiles of 256 x 256, eight waves of 128 rows by 64 channels, 64 terms at a time.  Memory writes a step's operands
-// straight into LDS, four steps of 32 KB in turn: while one is multiplied, the next one is read into registers, the one after it has landed or
-// is landing and the two behind that are asked for.  The copies are placed by hand (the compiler would wait for all of them before any read
-// of LDS): a wave waits until all but the two newest steps of its own have landed, then all waves meet; that one barrier a step also says that
+// The largest products: tiles of 32 TM rows by 256 channels, eight waves of 16 TM rows by 64 channels, 64 terms at a time.  Memory writes a step's
+// operands straight into LDS, four steps of up to 32 KB in turn: while one is multiplied, the next one is read into registers, the one after
+// it has landed or is landing and the two behind that are asked for.  The copies are placed by hand (the compiler would wait for all of them
+// before any read of LDS): a wave waits until all but the two newest steps of its own have landed, then all waves meet; that one barrier a step also says that
 // nobody reads the step that is written next any more.  LDS serves a wave's 16-byte reads in groups of 16 lanes, 0-3, 12-15, 20-23 and 24-27
 // first: with a piece at its place XOR `turned` of four rows' number, a group meets 16 different places of its 256 bytes (no conflicts counted).
 // Tiles are taken in bands of eight rows of tiles, so that the 32 that run on a die share their operands in its cache.
@@ -542,9 +544,11 @@ __device__ __forceinline__ i32x4 raw_rows(const int8_t *p, size_t ld, int row, i
     return (i32x4){(int)(uint32_t)at, (int)(uint32_t)(at >> 32) & 0xFFFF, left > 0x7FFFFF00ull ? 0x7FFFFF00 : (int)left, 0x00020000};
 }
 __device__ __forceinline__ int turned(int j) { return (0x78 >> 2 * j) & 3; }   // 0, 2, 3, 1
+template <int TM>
 __global__ __launch_bounds__(512) void k_linear_wide(LinearArgs a) {
-    constexpr int TM = 8, TN = 4, WM = 2, WN = 4, NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, STAGE = (BM + BN) * 64, STAGES = 4, CX = BM / 16 / NW, CW = BN / 16 / NW;
-    __shared__ __attribute__((aligned(1024))) int8_t lds[STAGES * STAGE];   // a stage: BM rows of 64 bytes, BN channels
+    constexpr int TN = 4, WM = 2, WN = 4, NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN, STAGE = (BM + BN) * 64, STAGES = 4;
+    constexpr int BLOCKS = (BM + BN) / 16, COPIES = (BLOCKS + NW - 1) / NW;   // a copy: 16 rows or channels; a wave's copies of a step
+    __shared__ __attribute__((aligned(1024))) int8_t lds[STAGES * STAGE + (BLOCKS % NW ? 1024 : 0)];   // a stage: BM rows of 64 bytes, BN channels
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
     const int nm = (a.rows + BM - 1) / BM, nn = (a.out + BN - 1) / BN, total = nm * nn * a.splits;
     int t = (int)blockIdx.x;
@@ -558,19 +562,23 @@ __global__ __launch_bounds__(512) void k_linear_wide(LinearArgs a) {
     const int m0 = (8 * band + t % bh) * BM, n0 = t / bh * BN;
     const int chunks = (a.in + 63) / 64, c0 = (int)((long)chunks * sp / a.splits), c1 = (int)((long)chunks * (sp + 1) / a.splits);
     const i32x4 xr = raw_rows(a.q, a.ldq, m0, a.rows, a.in), wr = raw_rows(a.w, a.ldw, n0, a.out, a.in);
-    unsigned o[CX + CW];
+    // rows past the last are the last (their products go nowhere); a wave's copy that is none copies nothing to where nobody reads
+    unsigned o[COPIES];
+    i32x4 from[COPIES];
 #pragma unroll
-    for (int i = 0; i < CX + CW; ++i) {
-        const unsigned piece = ((l & 3) ^ turned(l >> 4)) * 16;
-        if (i < CX) o[i] = (unsigned)min((wave * CX + i) * 16 + (l >> 2), a.rows - 1 - m0) * (unsigned)a.ldq + piece;
-        else o[i] = (unsigned)min((wave * CW + i - CX) * 16 + (l >> 2), a.out - 1 - n0) * (unsigned)a.ldw + piece;
+    for (int i = 0; i < COPIES; ++i) {
+        const int j = wave + NW * i;
+        const bool is_x = j < BM / 16;
+        const unsigned row = (is_x ? j : j - BM / 16) * 16 + (l >> 2), piece = ((l & 3) ^ turned(l >> 4)) * 16;
+        from[i] = is_x ? xr : wr;
+        o[i] = j >= BLOCKS ? OUTSIDE : is_x ? min(row, (unsigned)(a.rows - 1 - m0)) * (unsigned)a.ldq + piece : min(row, (unsigned)(a.out - 1 - n0)) * (unsigned)a.ldw + piece;
     }
     typedef __attribute__((address_space(3))) int8_t lds_byte;
     const unsigned base = (unsigned)(uintptr_t)(lds_byte *)lds;
     auto copy = [&](int c, int i) {
-        const unsigned k = min(c, c1 - 1) * 64, to = base + (c & (STAGES - 1)) * STAGE;
-        if (i < CX) copy_to_lds(xr, o[i] + k, to + (wave * CX + i) * 1024);
-        else copy_to_lds(wr, o[i] + k, to + BM * 64 + (wave * CW + i - CX) * 1024);
+        const unsigned k = min(c, c1 - 1) * 64;
+        const bool none = BLOCKS % NW && wave + NW * i >= BLOCKS;
+        copy_to_lds(from[i], o[i] + k, base + (none ? STAGES * STAGE : (c & (STAGES - 1)) * STAGE + (wave + NW * i) * 1024));
     };
     i32x4 acc[TN][TM];
 #pragma unroll
@@ -579,21 +587,21 @@ __global__ __launch_bounds__(512) void k_linear_wide(LinearArgs a) {
         for (int m = 0; m < TM; ++m) acc[n][m] = (i32x4){0, 0, 0, 0};
     const int wm = (wave % WM) * 16 * TM, wn = (wave / WM) * 16 * TN;
     const int at = li * 64 + ((lg ^ turned(li >> 2)) << 4);
-    auto meet = [&]() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * (CX + CW)) : "memory"); };
+    auto meet = [&]() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * COPIES) : "memory"); };
     i32x4 x[2][TM], w[2][TN];
     auto read_x = [&](int c, int m) { return *(const i32x4 *)(lds + (c & (STAGES - 1)) * STAGE + (wm + 16 * m) * 64 + at); };
     auto read_w = [&](int c, int n) { return *(const i32x4 *)(lds + (c & (STAGES - 1)) * STAGE + BM * 64 + (wn + 16 * n) * 64 + at); };
 #pragma unroll
     for (int p = 0; p < 3; ++p)
 #pragma unroll
-        for (int i = 0; i < CX + CW; ++i) copy(c0 + p, i);
+        for (int i = 0; i < COPIES; ++i) copy(c0 + p, i);
     meet();
 #pragma unroll
     for (int m = 0; m < TM; ++m) x[0][m] = read_x(c0, m);
 #pragma unroll
     for (int n = 0; n < TN; ++n) w[0][n] = read_w(c0, n);
 #pragma unroll
-    for (int i = 0; i < CX + CW; ++i) copy(c0 + 3, i);
+    for (int i = 0; i < COPIES; ++i) copy(c0 + 3, i);
     const int lim = min(a.in, c1 * 64);
     for (int c = c0; c < c1; c += 2)
 #pragma unroll
@@ -608,7 +616,7 @@ __global__ __launch_bounds__(512) void k_linear_wide(LinearArgs a) {
 #pragma unroll
             for (int n = 0; n < TN; ++n) {
 #pragma unroll
-                for (int i = n * (CX + CW) / TN; i < (n + 1) * (CX + CW) / TN; ++i) copy(cc + 4, i);
+                for (int i = n * COPIES / TN; i < (n + 1) * COPIES / TN; ++i) copy(cc + 4, i);
 #pragma unroll
                 for (int m = n * TM / TN; m < (n + 1) * TM / TN; ++m) x[u ^ 1][m] = read_x(cc + 1, m);
                 w[u ^ 1][n] = read_w(cc + 1, n);
@@ -648,17 +656,19 @@ template <int FORM, bool F32> void quantize(hipStream_t st, const QuantArgs &a, 
 
 constexpr int LONGEST = 1 << 26;   // rows or output channels: they are counted in 32 bits, and so are workgroups of up to 2^37 outputs
 struct Plan {
-    enum Form { ROWS, TILE128, TILE256 } form;
-    int units;    // ROWS: groups of 16 channels a workgroup
+    enum Form { ROWS, TILES, WIDE } form;
+    int units;    // ROWS: groups of 16 channels a workgroup; WIDE: 32 units rows a tile
     int splits;   // of the terms
 };
 // The launch that takes the least time by what each form takes on 256 compute units (us, measured at 4096 to 17920 terms):
 // Row groups, up to 64 rows: a round of compute units takes as long as a workgroup's channels, and as one group more for its beginning
 // and end.  26 x 22016 x 4096 with 1, 2, 3, 4, 6, 8 groups: 26.1, 24.0, 23.0, 25.9, 20.4, 20.3; 60 x 12288: 23.7, 21.1, 15.8, 17.1, 22.6, 27.2.
-// Tiles: of 128 x 128 a compute unit works on two at a time and takes 0.70 a chunk of 128 terms of each; of 256 x 256 on one, which takes 1.45
-// a chunk and 14 for its beginning and end.  Splitting the terms costs a second launch and the partial sums' way there and back.
-// 2000 x 22016 x 4096: 271 (128), 194 (256); 480 x 35840 x 6656: 167, 182; 2000 x 4096 x 4096: 46, 52; 480 x 6656 x 17920 with 1, 2, 3, 4, 6
-// splits: 105, 98, 103, 105, 106 and 203, 118, 95, 81, 115; 128 x 4096 x 4096: 28.5, 19.5, 16.5, 16.0, 15.2 and 49, 29, 24, 22, 21.
+// Tiles, over 128 terms at a time: of 128 x 128 a compute unit works on two at once, which take 1.17 for each, and 0.68 if there is one; of
+// 32 u x 256 on one, which takes 0.65 + 0.1 u; 8 and 14 for their beginning and end.  Splitting the terms costs a second launch and
+// the partial sums' way there and back.  Measured with 128 x 128 and with u = 5, 6, 7, 8: 2000 x 22016 x 4096 269, 244, 223, 232, 190;
+// 900 x 22016 x 4096 130, 130, 105, 112, 116; 480 x 35840 x 6656 170, 159, 154, 162, 182; 1500 x 6656 x 6656 102, 121, 78, 81, 85; 2000 x 4096
+// x 4096 46 and (u = 8) 52.  480 x 6656 x 17920 in 1, 2, 3, 4, 6 parts: 104, 96, 102, 105, 106 and (u = 8) 199, 116, 95, 80, 117; 183 x 5120 x 6656:
+// 43, 29, 25, 30, 28 and (u = 6) 74, 47, 39, 34, 30.
 Plan plan_of(int rows, int out, int in) {
     Plan p{Plan::ROWS, 1, 1};
     if (rows <= 64) {
@@ -676,18 +686,17 @@ Plan plan_of(int rows, int out, int in) {
     }
     double best = 1e30;
     const int chunks = (in + 127) / 128;
-    for (Plan::Form f : {Plan::TILE128, Plan::TILE256}) {
-        const int side = f == Plan::TILE128 ? 128 : 256;
-        const double tiles = (double)((rows + side - 1) / side) * ((out + side - 1) / side);
+    for (int u = 4; u <= 8; ++u) {   // 4: tiles of 128 x 128
+        const int high = 32 * u, across = u == 4 ? 128 : 256;
+        const double tiles = (double)((rows + high - 1) / high) * ((out + across - 1) / across);
         for (int s = 1; s <= 16 && s <= chunks; ++s) {
             if (s > 1 && (double)rows * out > (1 << 30)) break;   // (joined by outputs counted in 32 bits)
-            const double chunk = (chunks + s - 1) / s, rounds = tiles * s / 256;
-            const double us = (f == Plan::TILE128 ? std::max(rounds, 1.0) * chunk * 0.70 + 8.0 : std::ceil(rounds) * (chunk * 1.45 + 14.0)) +
-                              (s > 1 ? 4.0 + (double)s * rows * out * 8 / 1e7 : 0.0);
+            const double chunk = (chunks + s - 1) / s, turns = std::ceil(tiles * s / 256), pairs = std::floor(turns / 2);
+            const double us = (u == 4 ? pairs * (chunk * 1.17 + 8.0) + (turns - 2 * pairs) * (chunk * 0.68 + 8.0) : turns * (chunk * (0.65 + 0.10 * u) + 14.0)) +
+                              (s > 1 ? 2.0 + (double)s * rows * out * 8 / 1e7 : 0.0);
             if (us < best) {
                 best = us;
-                p.form = f;
-                p.splits = s;
+                p = {u == 4 ? Plan::TILES : Plan::WIDE, u, s};
             }
         }
     }
@@ -707,6 +716,9 @@ template <int MT> void rows_by_units(hipStream_t st, const LinearArgs &a, int un
     default: if constexpr (MT < 4) rows_launch<8, MT, MT == 1 ? 3 : 5>(st, a); break;
     }
 }
+template <int TM> void wide_launch(hipStream_t st, const LinearArgs &a) {
+    k_linear_wide<TM><<<(a.rows + 32 * TM - 1) / (32 * TM) * ((a.out + 255) / 256) * a.splits, 512, 0, st>>>(a);
+}
 void launch_linear(hipStream_t st, const LinearArgs &a, const Plan &p) {
     if (p.form == Plan::ROWS) {
         if (a.rows <= 16) rows_by_units<1>(st, a, p.units);
@@ -714,8 +726,11 @@ void launch_linear(hipStream_t st, const LinearArgs &a, const Plan &p) {
         else rows_by_units<4>(st, a, p.units);
         return;
     }
-    if (p.form == Plan::TILE128) k_linear_tiles<<<(a.rows + 127) / 128 * ((a.out + 127) / 128) * a.splits, 256, 0, st>>>(a);
-    else k_linear_wide<<<(a.rows + 255) / 256 * ((a.out + 255) / 256) * a.splits, 512, 0, st>>>(a);
+    if (p.form == Plan::TILES) k_linear_tiles<<<(a.rows + 127) / 128 * ((a.out + 127) / 128) * a.splits, 256, 0, st>>>(a);
+    else if (p.units == 5) wide_launch<5>(st, a);
+    else if (p.units == 6) wide_launch<6>(st, a);
+    else if (p.units == 7) wide_launch<7>(st, a);
+    else wide_launch<8>(st, a);
     if (a.splits > 1) k_linear_join<<<(unsigned)(((size_t)a.rows * ((a.out + 3) / 4) + 255) / 256), 256, 0, st>>>(a);
 }
 
@@ -772,8 +787,7 @@ koala_status koala_linear_quantized(void *hip_stream, int rows, int out_features
     if (q_stride > (1 << 22) || w_stride > (1 << 22)) return KOALA_E_SHAPE;   // 256 rows' bytes are counted in 31 bits
     if (need > 0 && (!workspace || workspace_bytes < need)) return KOALA_E_WORKSPACE;
     const Plan p = plan_of(rows, out_features, in_features);
-    const bool vec = y_stride % 4 == 0 && (uintptr_t)y % (4 * unit) == 0 && (uintptr_t)add % (4 * unit) == 0;
-    LinearArgs a{q, w, (size_t)q_stride, (size_t)w_stride, (size_t)y_stride, q_scale, w_scale, add, y, rows, out_features, in_features, y_dtype == KOALA_FP32, vec,
+    LinearArgs a{q, w, (size_t)q_stride, (size_t)w_stride, (size_t)y_stride, q_scale, w_scale, add, y, rows, out_features, in_features, y_dtype == KOALA_FP32,
                  p.splits, (int *)workspace};
     hipStream_t st = (hipStream_t)hip_stream;
     launch_linear(st, a, p);

@@ -122,10 +122,11 @@ def test_products(f32, rows, out, cols):
     assert (wide[:, :3] == 5).all() and (wide[:, 3 + out:] == 5).all()
 
 
-@pytest.mark.parametrize("rows,out,cols", [(2047, 8001, 4144), (1999, 4095, 11056), (700, 6650, 12304), (1023, 3999, 9040), (2000, 8192, 1088)])
+@pytest.mark.parametrize("rows,out,cols", [(2047, 8001, 4144), (1999, 4095, 11056), (700, 6650, 12304), (1023, 3999, 9040), (2000, 8192, 1088),
+                                           (160, 9001, 6672), (289, 6145, 11040), (1499, 6650, 6672), (217, 12289, 17936), (899, 5501, 4112)])
 def test_products_of_many_rows(rows, out, cols):
-    """Tiles of 256 by 256 in one, two, three or four parts of the sums, with an odd number of steps and ends inside of them; whatever
-    stands behind a row's end takes no part."""
+    """Tiles of 128 to 256 rows, one to seven parts of the sums, an odd number of steps and ends inside of them; whatever stands behind a
+    row's end takes no part."""
     import torch
     rng = np.random.default_rng(rows)
     q, w = (rng.integers(-128, 128, (n, cols + 16), dtype=np.int8) for n in (rows, out))

@@ -29,8 +29,9 @@ def test_no_kernel_spills_or_uses_packed_fp32(source, least):
         assert not any(re.search(r"\bv_pk_(add|mul|fma)_f32\b", l) for l in body), f"{name} uses packed fp32"
 
 
-def test_the_largest_products_main_loop_holds_what_its_waits_count_on():
-    name, (body, _) = next((n, k) for n, k in _kernels(_assembly("koala_int8")).items() if "k_linear_wide" in n)
+@pytest.mark.parametrize("tm", [5, 6, 7, 8])
+def test_the_largest_products_main_loop_holds_what_its_waits_count_on(tm):
+    body, _ = next(k for n, k in _kernels(_assembly("koala_int8")).items() if f"k_linear_wideILi{tm}E" in n)
     code = [re.sub(r"\s+", " ", l.split("//")[0].strip()) for l in body]
     code = [l for l in code if l and l[0] not in ";." and not l.endswith(":")]
     meets = [i for i, l in enumerate(code) if l == "s_waitcnt vmcnt(8) lgkmcnt(0)" and code[i + 1] == "s_barrier"]
@@ -41,8 +42,8 @@ def test_the_largest_products_main_loop_holds_what_its_waits_count_on():
     loop = code[meets[0]:end]                    # a step read and one copied before the turns, then two steps a turn, two products' worth
     memory = [l for l in loop if re.match(r"(buffer|global|flat|scratch)_", l)]
     assert len(memory) == 12 and all(l.startswith("buffer_load_dwordx4") and l.endswith("lds") for l in memory), memory
-    assert sum(l.startswith("ds_read_b128") for l in loop) == 36
-    assert sum(l.startswith("v_mfma_i32_16x16x64_i8") for l in loop) == 64
-    assert not any(re.match(r"ds_(write|bpermute|swizzle)|s_(load|buffer_load)|v_(readlane|readfirstlane)", l) for l in loop)
+    assert sum(l.startswith("ds_read_b128") for l in loop) == 3 * (tm + 4)
+    assert sum(l.startswith("v_mfma_i32_16x16x64_i8") for l in loop) == 2 * 4 * tm
+    assert not any(re.match(r"ds_(write|bpermute|swizzle)|s_(load|buffer_load)|v_(readlane|readfirstlane)", l) for l in code[meets[0]:copies[-1]])
     for i in copies:                             # a copy's place in LDS is set right before it
         assert code[i - 2].startswith("s_mov_b32 m0,") and code[i - 1] == "s_nop 4"
