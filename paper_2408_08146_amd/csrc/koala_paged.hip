@@ -765,7 +765,7 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
     float M = -INFINITY, L = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
-    constexpr int PARTS = 4;   // requested at once
+    constexpr int PARTS = 8;   // requested at once
     for (int w = w0; w <= w1; w += PARTS) {
         float m[PARTS], ls[PARTS];
         f32x4 x[PARTS][E / 4];
@@ -856,11 +856,12 @@ int compute_units() {
 enum { ATTEND_WGS_MAX = 512 };   // what the workspace is sized for
 
 // Whether every item is left to one workgroup, which spares the second launch and the parts' way through memory: where all items run at
-// once, until dividing them among the idle compute units pays.  us whole and divided, heads of 128, over 500, 1000, 2000, 3000, 4000 keys:
-// 32 items of one row 8.2, 9.5, 13.6, 17.3, 21.1 and 11.7, 12.2, 14.0, 14.2, 14.3; 64 items (26 rows) 8.4, 10.2, 14.4, 18.0, 22.0 and 14.4, 16.0,
-// 17.9, 18.7, 20.0; 240 items (26 rows) 8.5, 11.3, 18.6, 20.8, 26.1 and 17.4, 19.2, 21.5, 24.9, 27.2.  In more than one round only small items: 280
-// over 600, 1000, 3000 keys 13.6, 18.7, 36.3 and 15.4, 18.3, 28.0; 1200 35.8, 47.5, 104.5 and 35.3, 41.9, 97.3.
-bool attend_whole(int items, int steps, int cu) { return items <= cu ? steps <= 60 + items / 2 : items <= 4 * cu && steps <= 16; }
+// once, until dividing them among the idle compute units pays.  us whole and divided, heads of 128, over 1000, 1500, 2000, 3000, 4000 keys:
+// one item of one row 9.0, 10.7, 12.8, 16.5, 20.3 and 9.7, 10.3, 10.7, 11.7, 12.3; 32 items 9.6, 11.4, 13.5, 17.3, 21.1 and 12.0, 13.6, 13.6, 13.5, 13.7;
+// 64 (26 rows) 10.1, 12.2, 14.4, 18.1, 21.9 and 16.0, 16.8, 17.6, 18.3, 19.5; 128 9.4, 11.3, 13.8, 17.9, 22.1 and 14.0, 15.5, 16.1, 19.3, 21.7; 240
+// 10.0, 14.1, 16.7, 21.1, 25.9 and 16.7, 19.5, 22.1, 25.7, 29.8.  In more than one round only small items: 280 over 600, 1000, 3000 keys 13.6,
+// 18.7, 36.3 and 15.4, 18.3, 28.0; 1200 35.8, 47.5, 104.5 and 35.3, 41.9, 97.3.
+bool attend_whole(int items, int steps, int cu) { return items <= cu ? steps <= 44 + items * 5 / 8 : items <= 4 * cu && steps <= 16; }
 
 template <int DH, int MT, bool F32>
 void launch_attend(hipStream_t st, const AttendArgs &a, int cu) {
