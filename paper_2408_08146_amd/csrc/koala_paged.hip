@@ -67,7 +67,8 @@ template <bool F32> __device__ __forceinline__ void store8(void *dst, size_t i, 
 // Append.  A lane holds eight dimensions of a head's first half and their rotary partners in the second, so a rotation needs no
 // exchange and a block of 32 is four neighbouring lanes.  A row's queries, keys and values are its n_heads + 2 n_kv heads in turn.
 // The rotation is computed product by product, without fused multiply-adds: a code then does not depend on how a compiler
-// contracts a sum.
+// contracts a sum.  Bound by memory: 8000 rows of 40 + 8 + 8 heads of 128 in bfloat16 36 us, 205 MB at 5.7 TB/s; 26 rows of 96 heads 3.4 us, a
+// launch and the way from a length over a page to a row.
 // ---------------------------------------------------------------------------------------------
 struct AppendArgs {
     Pool p;
@@ -155,7 +156,8 @@ template <int DH, bool F32> __global__ __launch_bounds__(256) void k_paged_appen
 }
 
 // ---------------------------------------------------------------------------------------------
-// Read back: eight values a lane
+// Read back: eight values a lane, keys and values.  Bound by memory: 32000 slots of 8 heads of 128 28 us, 166 MB at 5.8 TB/s; 8000
+// 10.4 us.  Two or four of these a lane, all asked for at once, are no faster, and slower where there are few.
 // ---------------------------------------------------------------------------------------------
 struct ReadArgs {
     Pool p;
@@ -205,6 +207,8 @@ template <int DH, bool F32> __global__ __launch_bounds__(256) void k_paged_read(
 // ---------------------------------------------------------------------------------------------
 // Commit.  A lane moves one 16-byte piece (or the exponents) of every accepted row of a key head, in path order: node ids grow
 // along a path, so the slot a row moves to (its place on the path) is never one that a later row still has to be read from.
+// Eight rows' pieces are asked for at once, their slots' pages with the lengths.  Bound by that chain of three reads: 32 layers, 8 sequences,
+// 32 heads, paths of 4: 6 us; 3 layers of one sequence 3.1.
 // ---------------------------------------------------------------------------------------------
 struct CommitArgs {
     Pool p;
@@ -272,6 +276,13 @@ __global__ void k_paged_advance(int32_t *len, const int32_t *accept_len, int bat
 // outputs P and V are fp16: V is exact as long as its exponents are in range (a wave that meets one that is not does its steps again the
 // other way), P has 11 bits, an eighth of the output's own rounding.  For fp32 outputs, and where rows differ in what they see, V is
 // bfloat16, exact always, and P the sum of three bfloat16 pieces; so are fp32 queries.  bfloat16 queries are exact.
+//
+// What bounds it: with one row tile memory (8 sequences, 8 key heads of 8 query heads, 26000 keys on average: 46 us and 4.5 for the join, 230 MB
+// at 5.0 TB/s while it runs); with two the instructions of two waves a SIMD (8 sequences, 52 heads, 60 rows, 4400 keys: 110 us; the matrix pipe
+// is busy for a quarter of them, the vector unit for 45%, loads that always hit the cache would take 101); with few items the chain from
+// lengths over pages to codes, and the waves' meeting (32 items of one row over 777 keys 8.5 us).  Tried at the two tiles without a gain:
+// the next step's values beside this one's products in a second buffer, LDS layouts without bank conflicts, queries in registers, pages looked
+// up further ahead, one tile with three or four waves a SIMD (157 us), four tiles with one (142), more workgroups than run at once (119 to 139).
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 typedef u32x4 __attribute__((may_alias)) u32x4_alias;
@@ -744,7 +755,8 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, 2) void k_paged_attend(At
 }
 
 // Joins the partial results of the items that more than one workgroup has worked on.  A workgroup an item and row tile, a lane
-// DH / 16 dimensions of a row.
+// DH / 16 dimensions of a row.  Bound by the reads' way, one behind another: 64 items in eight or nine parts 4.5 us; eight parts at once and
+// not four take 1 us from an item in 32 (one head over 30000 keys 17.1, 16.1 us with the attention).  1664 row tiles, few of them in parts, 7.5 us.
 template <int DH, int MT, bool F32>
 __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
     constexpr int E = DH / 16;
