@@ -278,11 +278,11 @@ __global__ void k_paged_advance(int32_t *len, const int32_t *accept_len, int bat
 // bfloat16, exact always, and P the sum of three bfloat16 pieces; so are fp32 queries.  bfloat16 queries are exact.
 //
 // What bounds it: with one row tile memory (8 sequences, 8 key heads of 8 query heads, 26000 keys on average: 46 us and 4.5 for the join, 230 MB
-// at 5.0 TB/s while it runs); with two the instructions of two waves a SIMD (8 sequences, 52 heads, 60 rows, 4400 keys: 110 us; the matrix pipe
-// is busy for a quarter of them, the vector unit for 45%, loads that always hit the cache would take 101); with few items the chain from
-// lengths over pages to codes, and the waves' meeting (32 items of one row over 777 keys 8.5 us).  Tried at the two tiles without a gain:
-// the next step's values beside this one's products in a second buffer, LDS layouts without bank conflicts, queries in registers, pages looked
-// up further ahead, one tile with three or four waves a SIMD (157 us), four tiles with one (142), more workgroups than run at once (119 to 139).
+// at 5.0 TB/s while it runs); with two the instructions of two waves a SIMD (8 sequences, 52 heads, 60 rows, 4400 keys: 109 us; the matrix pipe
+// is busy for a quarter of them, the vector unit for 45%, loads that always hit the cache take 13% less); with few items the chain from
+// lengths over pages to codes, and the waves' meeting (32 items of one row over 777 keys 8.3 us).  Tried at the two tiles without a gain:
+// the next step's values beside this one's products in a second buffer, LDS layouts without bank conflicts, queries in registers, one tile with
+// three or four waves a SIMD (157 us), four tiles with one (142), more workgroups than run at once (119 to 139).
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 typedef u32x4 __attribute__((may_alias)) u32x4_alias;
@@ -399,8 +399,9 @@ __device__ __forceinline__ Shares count_steps(const AttendArgs &a, int l) {
     return s;
 }
 
-// Steps whose codes a wave has under way besides the one it works on
-constexpr int ahead(int MT, bool F32) { return MT == 2 ? 3 : F32 ? 2 : 3; }
+// Steps whose codes a wave has under way besides the one it works on; even, since their scores take turns in two sets of registers.  (Three
+// are no faster where steps are many, and where they are few it is more to ask for before the first: 32 heads, 26 rows, 1050 keys 10.5, 9.4 us.)
+constexpr int AHEAD = 2;
 
 // WHOLE: every item is one workgroup's, of eight waves; the grid is the items
 template <int DH, int MT, bool F32, bool WHOLE>
@@ -413,7 +414,6 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, 2) void k_paged_attend(At
     __shared__ float mm[NW][16][2];
     constexpr bool QLDS = MT == 2;         // two tiles' queries are kept in LDS: the registers hold codes instead
     __shared__ u32x4 qs[QLDS ? MT * KS * 64 : 1];
-    constexpr int AHEAD = ahead(MT, F32);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
     unsigned char *vt = vt_all + wave * STEP * VS;
 
@@ -631,8 +631,8 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, 2) void k_paged_attend(At
         // A step whose keys every row sees, its scores there already; V and P in fp16 where the output is bfloat16.  The next step's scores
         // are taken beside this one's powers and products: neither waits for the other.
         unsigned beyond = 0;   // whether a value was outside fp16's range: then it is all done again
-        f32x4 sc[2][MT];
-        auto full_step = [&](const Codes<CW> &c, const Codes<CW> &next) {
+        f32x4 scs[2][2][MT];
+        auto full_step = [&](const Codes<CW> &c, const Codes<CW> &next, f32x4 (*sc)[MT], f32x4 (*sc_next)[MT]) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const float s = exp_scale(c.ve[j]);
@@ -648,7 +648,7 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, 2) void k_paged_attend(At
 #pragma unroll
                 for (int e = 0; e < 8; ++e) p[mt][e] = sc[e >> 2][mt][e & 3];
             maxima(p, shift);
-            scores(next, sc);
+            scores(next, sc_next);
             f16x8 ph[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -670,22 +670,24 @@ __global__ __launch_bounds__(WHOLE ? 512 : 64 * WAVES, 2) void k_paged_attend(At
         const int st = s0 + wave, mine = (last - st + NW - 1) / NW;
         const int open = min(mine, max(0, (min(ctx, kv_end) / STEP - st + NW - 1) / NW));   // those that every row sees
         if (mine > 0) {
-            int page[AHEAD + 1][2], page_end[2];
+            int page[AHEAD][2], page_end[2];
             Codes<CW> c[AHEAD], c_end;
             find(page_end, st + (mine - 1) * NW);
 #pragma unroll
-            for (int u = 0; u <= AHEAD; ++u) find(page[u], st + u * NW);
+            for (int u = 0; u < AHEAD; ++u) find(page[u], st + u * NW);
             fetch(c_end, page_end, st + (mine - 1) * NW);
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) fetch(c[u], page[u], st + u * NW);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) find(page[u], st + (u + AHEAD) * NW);
             if (open < mine) any_step(c_end, st + (mine - 1) * NW);
-            scores(c[0], sc);
+            scores(c[0], scs[0]);
             for (int i = 0; i < open; i += AHEAD)
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u) {
-                    if (i + u < open) full_step(c[u], c[(u + 1) % AHEAD]);
-                    fetch(c[u], page[AHEAD], st + (i + u + AHEAD) * NW);
-                    find(page[AHEAD], st + (i + u + AHEAD + 1) * NW);
+                    if (i + u < open) full_step(c[u], c[(u + 1) % AHEAD], scs[u & 1], scs[u & 1 ^ 1]);
+                    fetch(c[u], page[u], st + (i + u + AHEAD) * NW);
+                    find(page[u], st + (i + u + 2 * AHEAD) * NW);
                 }
             // values outside fp16's range, or more than one step to be masked (a cut-off sequence): step by step
             const bool again = !F32 && __builtin_amdgcn_ballot_w64(beyond) != 0;
@@ -869,11 +871,12 @@ enum { ATTEND_WGS_MAX = 512 };   // what the workspace is sized for
 
 // Whether every item is left to one workgroup, which spares the second launch and the parts' way through memory: where all items run at
 // once, until dividing them among the idle compute units pays.  us whole and divided, heads of 128, over 1000, 1500, 2000, 3000, 4000 keys:
-// one item of one row 9.0, 10.7, 12.8, 16.5, 20.3 and 9.7, 10.3, 10.7, 11.7, 12.3; 32 items 9.6, 11.4, 13.5, 17.3, 21.1 and 12.0, 13.6, 13.6, 13.5, 13.7;
-// 64 (26 rows) 10.1, 12.2, 14.4, 18.1, 21.9 and 16.0, 16.8, 17.6, 18.3, 19.5; 128 9.4, 11.3, 13.8, 17.9, 22.1 and 14.0, 15.5, 16.1, 19.3, 21.7; 240
-// 10.0, 14.1, 16.7, 21.1, 25.9 and 16.7, 19.5, 22.1, 25.7, 29.8.  In more than one round only small items: 280 over 600, 1000, 3000 keys 13.6,
-// 18.7, 36.3 and 15.4, 18.3, 28.0; 1200 35.8, 47.5, 104.5 and 35.3, 41.9, 97.3.
-bool attend_whole(int items, int steps, int cu) { return items <= cu ? steps <= 44 + items * 5 / 8 : items <= 4 * cu && steps <= 16; }
+// one item of one row 8.4, 10.1, 12.0, 15.8, 19.3 and 9.4, 9.7, 10.0, 10.9, 11.6; 32 items 8.8, 10.7, 12.5, 16.4, 20.1 and 11.1, 12.3, 12.4, 12.9,
+// 13.4; 64 (26 rows) 9.4, 11.7, 13.4, 17.4, 21.2 and 15.3, 16.1, 16.8, 17.6, 18.9; 128 8.6, 10.7, 12.9, 17.0, 21.0 and 13.2, 14.8, 16.4, 18.5, 20.7; 240
+// 9.5, 12.7, 14.9, 19.3, 23.8 and 16.0, 18.5, 20.9, 24.5, 28.8.  In more than one round the fewer the longer: over 300, 500, 700, 900, 1100 keys 280 items
+// 10.9, 11.9, 13.6, 16.5, 17.3 and 13.1, 13.6, 15.7, 16.7, 18.5; 640 15.4, 20.1, 23.0, 26.7, 26.3 and 17.6, 20.6, 23.3, 25.8, 28.1; 840 (60 rows) 34.1, 40.0,
+// 44.4, 48.8, 54.1 and 29.3, 34.1, 39.0, 42.2, 48.0; 1000 21.6, 26.7, 30.7, 35.8, 35.5 and 22.5, 25.8, 29.5, 33.3, 36.0.
+bool attend_whole(int items, int steps, int cu) { return steps <= (items <= cu ? 44 + items * 5 / 8 : 40 - items / 28); }
 
 template <int DH, int MT, bool F32>
 void launch_attend(hipStream_t st, const AttendArgs &a, int cu) {
