@@ -663,6 +663,7 @@ struct Plan {
 // The launch that takes the least time by what each form takes on 256 compute units (us, measured at 4096 to 17920 terms):
 // Row groups, up to 64 rows: a round of compute units takes as long as a workgroup's channels, and as one group more for its beginning
 // and end.  26 x 22016 x 4096 with 1, 2, 3, 4, 6, 8 groups: 26.1, 24.0, 23.0, 25.9, 20.4, 20.3; 60 x 12288: 23.7, 21.1, 15.8, 17.1, 22.6, 27.2.
+// (Three tiles of rows where four are not needed: 40 x 22016 x 4096 25.4, 21.3; 40 x 4096 x 4096 8.7, 8.0.)
 // Tiles, over 128 terms at a time: of 128 x 128 a compute unit works on two at once, which take 1.17 for each, and 0.68 if there is one; of
 // 32 u x 256 on one, which takes 0.65 + 0.1 u; 8 and 14 for their beginning and end.  Splitting the terms costs a second launch and
 // the partial sums' way there and back.  Measured with 128 x 128 and with u = 5, 6, 7, 8: 2000 x 22016 x 4096 269, 244, 223, 232, 190;
@@ -709,11 +710,11 @@ template <int U, int MT, int AHEAD> void rows_launch(hipStream_t st, const Linea
 template <int MT> void rows_by_units(hipStream_t st, const LinearArgs &a, int units) {
     switch (units) {
     case 1: rows_launch<1, MT, 1 + MT>(st, a); break;
-    case 2: rows_launch<2, MT, MT == 1 ? 3 : MT == 2 ? 4 : 3>(st, a); break;
-    case 3: rows_launch<3, MT, MT == 1 ? 4 : MT == 2 ? 5 : 7>(st, a); break;
-    case 4: rows_launch<4, MT, MT == 1 ? 5 : MT == 2 ? 6 : 4>(st, a); break;
-    case 6: rows_launch<6, MT, MT == 1 ? 7 : MT == 2 ? 4 : 5>(st, a); break;
-    default: if constexpr (MT < 4) rows_launch<8, MT, MT == 1 ? 3 : 5>(st, a); break;
+    case 2: rows_launch<2, MT, MT == 1 ? 3 : MT == 2 ? 4 : MT == 3 ? 5 : 3>(st, a); break;
+    case 3: rows_launch<3, MT, MT == 1 ? 4 : MT == 2 ? 5 : MT == 3 ? 6 : 7>(st, a); break;
+    case 4: rows_launch<4, MT, MT == 1 ? 5 : MT == 2 ? 6 : MT == 3 ? 7 : 4>(st, a); break;
+    case 6: rows_launch<6, MT, MT == 1 ? 7 : MT == 2 ? 4 : MT == 3 ? 3 : 5>(st, a); break;
+    default: if constexpr (MT < 3) rows_launch<8, MT, MT == 1 ? 3 : 5>(st, a); break;
     }
 }
 template <int TM> void wide_launch(hipStream_t st, const LinearArgs &a) {
@@ -723,6 +724,7 @@ void launch_linear(hipStream_t st, const LinearArgs &a, const Plan &p) {
     if (p.form == Plan::ROWS) {
         if (a.rows <= 16) rows_by_units<1>(st, a, p.units);
         else if (a.rows <= 32) rows_by_units<2>(st, a, p.units);
+        else if (a.rows <= 48) rows_by_units<3>(st, a, p.units);
         else rows_by_units<4>(st, a, p.units);
         return;
     }

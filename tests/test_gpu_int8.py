@@ -122,6 +122,21 @@ def test_products(f32, rows, out, cols):
     assert (wide[:, :3] == 5).all() and (wide[:, 3 + out:] == 5).all()
 
 
+@pytest.mark.parametrize("rows", [1, 20, 40, 60])
+@pytest.mark.parametrize("out", [6650, 11003, 16000, 22001, 32000])
+def test_products_of_many_channels(rows, out):
+    """Two to eight groups of 16 channels a workgroup, one to four tiles of rows, a last run that ends early, rows among wider ones."""
+    import torch
+    rng = np.random.default_rng(rows + out)
+    q, w = (dev(rng.integers(-128, 128, (n, 2832 + 16), dtype=np.int8)) for n in (rows, out))
+    q, w = q[:, :2832], w[:, :2832]
+    qs, ws = (np.exp(rng.standard_normal(n)).astype(np.float32) * 0.01 for n in (rows, out))
+    want = ((q.double() @ w.double().T) * dev(qs).double()[:, None] * dev(ws).double()).cpu().numpy()   # the sums are exact
+    y = torch.full((rows, out), 7.0, device="cuda")
+    QuantizedLinear(w, dev(ws)).forward(q, dev(qs), y)
+    assert agrees(y, want, 4 * 2.0 ** -24 * np.abs(want), True)
+
+
 @pytest.mark.parametrize("rows,out,cols", [(2047, 8001, 4144), (1999, 4095, 11056), (700, 6650, 12304), (1023, 3999, 9040), (2000, 8192, 1088),
                                            (160, 9001, 6672), (289, 6145, 11040), (1499, 6650, 6672), (217, 12289, 17936), (899, 5501, 4112)])
 def test_products_of_many_rows(rows, out, cols):
