@@ -83,7 +83,8 @@ template <bool F32> struct Eight {
     }
 };
 template <bool F32> __device__ __forceinline__ rsrc_t row_of(const void *src, size_t row, int n) {   // an odd last bfloat16 is not part of it
-    return __builtin_amdgcn_make_buffer_rsrc(F32 ? (void *)((float *)src + row) : (void *)((bf16_t *)src + row), 0, F32 ? 4 * n : 2 * n & ~3, 0x00020000);
+    void *const p = F32 ? (void *)((float *)src + row) : (void *)((bf16_t *)src + row);
+    return __builtin_amdgcn_make_buffer_rsrc(p, 0, F32 ? 4 * n : 2 * n & ~3, 0x00020000);
 }
 template <bool F32> __device__ __forceinline__ Eight<F32> eight_of(rsrc_t rsrc, const void *src, size_t row, int i, int n) {
     Eight<F32> r;
@@ -99,7 +100,9 @@ template <bool F32> __device__ __forceinline__ Eight<F32> eight_of(rsrc_t rsrc, 
 }
 
 // over the 64 lanes of a wave, in all of them
-template <int CTRL> __device__ __forceinline__ uint32_t turned_row(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
+template <int CTRL> __device__ __forceinline__ uint32_t turned_row(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
 template <class F> __device__ __forceinline__ uint32_t over_row(uint32_t x, F f) {   // 16 lanes: each 8, 4, 2, 1 further on
     x = f(x, turned_row<0x128>(x));
     x = f(x, turned_row<0x124>(x));
@@ -198,7 +201,8 @@ __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
                 take(c, v[0]);
                 add(v[0]);
             }
-        sum = __uint_as_float(over_workgroup(__float_as_uint(sum), s_sum, [](uint32_t x, uint32_t y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); }));
+        const auto plus = [](uint32_t x, uint32_t y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); };
+        sum = __uint_as_float(over_workgroup(__float_as_uint(sum), s_sum, plus));
         r = 1.f / sqrtf(sum / (float)cols + a.eps);
     }
     auto scaled = [&](float *x, const float *g) {
@@ -253,7 +257,8 @@ __global__ __launch_bounds__(1024) void k_quantize_rows(QuantArgs a) {
         }
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-            const uint32_t lo = __builtin_amdgcn_perm(d[4 * z + 1], d[4 * z], 0x0C0C0400), hi = __builtin_amdgcn_perm(d[4 * z + 3], d[4 * z + 2], 0x04000C0C);
+            const uint32_t lo = __builtin_amdgcn_perm(d[4 * z + 1], d[4 * z], 0x0C0C0400);
+            const uint32_t hi = __builtin_amdgcn_perm(d[4 * z + 3], d[4 * z + 2], 0x04000C0C);
             w[z] = bad ? 0u : lo | hi;
         }
         *(u32x2 *)(a.q + row * a.ldq + 8 * c) = (u32x2){w[0], w[1]};
@@ -335,7 +340,8 @@ template <int TM, int TN> __device__ __forceinline__ void finish_tile(const Line
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int i = 0; i < TM; ++i)
-                if (m + 16 * i < a.rows && n + 16 * j < a.out) *(i32x4 *)(a.part + ((size_t)split * a.rows + m + 16 * i) * ld + n + 16 * j) = acc[j][i];
+                if (m + 16 * i < a.rows && n + 16 * j < a.out)
+                    *(i32x4 *)(a.part + ((size_t)split * a.rows + m + 16 * i) * ld + n + 16 * j) = acc[j][i];
         return;
     }
     float qs[TM];
@@ -355,6 +361,9 @@ template <int TM, int TN> __device__ __forceinline__ void finish_tile(const Line
 // 16 channels an instruction, streams 4.4 to 5.1 TB/s here, runs of 1 KiB 6.2.  It turns a tile (16 rows or channels of a chunk) into
 // operands through LDS of its own (no barrier; 16-byte pieces at their place XOR the row's number).  A chunk is MT tiles of the rows,
 // kept as operands, and U of the weights; AHEAD tiles are under way in registers.
+// Bound by memory and by a round's beginning and end: 26 x 35840 x 6656 45.6 us, 5.2 TB/s; 26 x 22016 x 4096 20.2 us, 4.5 TB/s; 1 x 22016 x 4096 19.1;
+// 1 x 4096 x 4096 5.7.  Without a gain: 512 or 1024 terms a run, sixteen waves, the rows' operands loaded as the matrix pipe wants them (60 x 12288
+// x 4096 15.8, 18.1), the last round's groups spread over all compute units.
 template <int U, int MT, int AHEAD>
 __global__ __launch_bounds__(512) void k_linear_rows(LinearArgs a) {
     constexpr int KC = 256, NW = 8, KS = KC / 64, LD = KC / 64, V = U + MT;   // LD: loads a tile is
@@ -458,7 +467,8 @@ __global__ __launch_bounds__(512) void k_linear_rows(LinearArgs a) {
 // modulo 8: a wave's reads then meet different banks.  480 x 35840 x 6656: 167 us, 1.37 POP/s; what bounds it is the wait for LDS and the
 // other waves in every step.
 __global__ __launch_bounds__(256) void k_linear_tiles(LinearArgs a) {
-    constexpr int TM = 4, TN = 4, WM = 2, WN = 2, AHEAD = 3, NT = 64 * WM * WN, RPT = NT / 8, BM = 16 * TM * WM, BN = 16 * TN * WN, LX = BM / RPT, LW = BN / RPT;   // 16-byte loads a thread
+    constexpr int TM = 4, TN = 4, WM = 2, WN = 2, AHEAD = 3, NT = 64 * WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN;
+    constexpr int RPT = NT / 8, LX = BM / RPT, LW = BN / RPT;   // rows a load of the workgroup is, a thread's loads
     __shared__ __attribute__((aligned(16))) int8_t sx[2][BM * 128], sw[2][BN * 128];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
     const int nm = (a.rows + BM - 1) / BM, nn = (a.out + BN - 1) / BN, total = nm * nn * a.splits;
@@ -571,7 +581,8 @@ __global__ __launch_bounds__(512) void k_linear_wide(LinearArgs a) {
         const bool is_x = j < BM / 16;
         const unsigned row = (is_x ? j : j - BM / 16) * 16 + (l >> 2), piece = ((l & 3) ^ turned(l >> 4)) * 16;
         from[i] = is_x ? xr : wr;
-        o[i] = j >= BLOCKS ? OUTSIDE : is_x ? min(row, (unsigned)(a.rows - 1 - m0)) * (unsigned)a.ldq + piece : min(row, (unsigned)(a.out - 1 - n0)) * (unsigned)a.ldw + piece;
+        const unsigned last = (unsigned)(is_x ? a.rows - 1 - m0 : a.out - 1 - n0), ld = (unsigned)(is_x ? a.ldq : a.ldw);
+        o[i] = j >= BLOCKS ? OUTSIDE : min(row, last) * ld + piece;
     }
     typedef __attribute__((address_space(3))) int8_t lds_byte;
     const unsigned base = (unsigned)(uintptr_t)(lds_byte *)lds;
@@ -628,7 +639,7 @@ __global__ __launch_bounds__(512) void k_linear_wide(LinearArgs a) {
     finish_tile<TM, TN>(a, sp, m0 + wm + li, n0 + wn + 4 * lg, acc);
 }
 
-// Sums of the splits, and the outputs: four a thread
+// Sums of the splits, and the outputs: four a thread.  Bound by memory: 480 x 6656 in four parts 10.3 us, 57 MB at 5.6 TB/s.
 __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
     const unsigned quads = (a.out + 3) / 4, at = blockIdx.x * 256 + threadIdx.x, row = at / quads, quad = at - row * quads;
     if (row >= (unsigned)a.rows) return;
@@ -693,7 +704,8 @@ Plan plan_of(int rows, int out, int in) {
         for (int s = 1; s <= 16 && s <= chunks; ++s) {
             if (s > 1 && (double)rows * out > (1 << 30)) break;   // (joined by outputs counted in 32 bits)
             const double chunk = (chunks + s - 1) / s, turns = std::ceil(tiles * s / 256), pairs = std::floor(turns / 2);
-            const double us = (u == 4 ? pairs * (chunk * 1.17 + 8.0) + (turns - 2 * pairs) * (chunk * 0.68 + 8.0) : turns * (chunk * (0.65 + 0.10 * u) + 14.0)) +
+            const double us = (u == 4 ? pairs * (chunk * 1.17 + 8.0) + (turns - 2 * pairs) * (chunk * 0.68 + 8.0)
+                                      : turns * (chunk * (0.65 + 0.10 * u) + 14.0)) +
                               (s > 1 ? 2.0 + (double)s * rows * out * 8 / 1e7 : 0.0);
             if (us < best) {
                 best = us;
