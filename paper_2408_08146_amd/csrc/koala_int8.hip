@@ -1,7 +1,6 @@
 // Projections in 8-bit integers with a scale for each token and each output channel (koala.h, "Projections in 8-bit integers").
 #include "koala_internal.h"
 #include <algorithm>
-#include <cmath>
 
 namespace {
 
@@ -673,7 +672,7 @@ struct Plan {
 };
 // The launch that takes the least time by what each form takes on 256 compute units (us, measured at 4096 to 17920 terms):
 // Row groups, up to 64 rows: a round of compute units takes as long as a workgroup's channels, and as one group more for its beginning
-// and end.  26 x 22016 x 4096 with 1, 2, 3, 4, 6, 8 groups: 26.1, 24.0, 23.0, 25.9, 20.4, 20.3; 60 x 12288: 23.7, 21.1, 15.8, 17.1, 22.6, 27.2.
+// and end.  26 x 22016 x 4096 with 1, 2, 3, 4, 6, 8 groups: 26.4, 21.8, 21.2, 24.3, 20.4, 21.7; 60 x 12288 x 4096: 23.4, 21.5, 16.5, 16.9, 22.4.
 // (Three tiles of rows where four are not needed: 40 x 22016 x 4096 25.4, 21.3; 40 x 4096 x 4096 8.7, 8.0.)
 // Tiles, over 128 terms at a time: of 128 x 128 a compute unit works on two at once, which take 1.17 for each, and 0.68 if there is one; of
 // 32 u x 256 on one, which takes 0.65 + 0.1 u; 8 and 14 for their beginning and end.  Splitting the terms costs a second launch and
@@ -700,12 +699,12 @@ Plan plan_of(int rows, int out, int in) {
     const int chunks = (in + 127) / 128;
     for (int u = 4; u <= 8; ++u) {   // 4: tiles of 128 x 128
         const int high = 32 * u, across = u == 4 ? 128 : 256;
-        const double tiles = (double)((rows + high - 1) / high) * ((out + across - 1) / across);
+        const long tiles = (long)((rows + high - 1) / high) * ((out + across - 1) / across);
         for (int s = 1; s <= 16 && s <= chunks; ++s) {
-            if (s > 1 && (double)rows * out > (1 << 30)) break;   // (joined by outputs counted in 32 bits)
-            const double chunk = (chunks + s - 1) / s, turns = std::ceil(tiles * s / 256), pairs = std::floor(turns / 2);
-            const double us = (u == 4 ? pairs * (chunk * 1.17 + 8.0) + (turns - 2 * pairs) * (chunk * 0.68 + 8.0)
-                                      : turns * (chunk * (0.65 + 0.10 * u) + 14.0)) +
+            if (s > 1 && (long)rows * out > 1 << 30) break;   // (joined by outputs counted in 32 bits)
+            const long turns = (tiles * s + 255) / 256;
+            const double chunk = (chunks + s - 1) / s, pairs = (double)(turns / 2), one = (double)(turns & 1);
+            const double us = (u == 4 ? pairs * (chunk * 1.17 + 8.0) + one * (chunk * 0.68 + 8.0) : (double)turns * (chunk * (0.65 + 0.10 * u) + 14.0)) +
                               (s > 1 ? 2.0 + (double)s * rows * out * 8 / 1e7 : 0.0);
             if (us < best) {
                 best = us;
@@ -714,6 +713,14 @@ Plan plan_of(int rows, int out, int in) {
         }
     }
     return p;
+}
+
+// the launch for these sizes and its workspace, or why there is none
+koala_status planned(int rows, int out, int in, Plan *p, size_t *bytes) {
+    if (rows < 1 || out < 1 || in < 16 || in % 16 || in > 131056 || rows > LONGEST || out > LONGEST || (long)rows * out > 1l << 37) return KOALA_E_SHAPE;
+    *p = plan_of(rows, out, in);
+    *bytes = p->splits > 1 ? (size_t)p->splits * rows * ((out + 3) / 4) * 16 : 0;
+    return KOALA_OK;
 }
 
 template <int U, int MT, int AHEAD> void rows_launch(hipStream_t st, const LinearArgs &a) {
@@ -777,12 +784,8 @@ koala_status koala_quantize_rows(void *hip_stream, int form, int x_dtype, int ro
 
 koala_status koala_linear_workspace_bytes(int rows, int out_features, int in_features, size_t *out) {
     if (!out) return KOALA_E_NULL;
-    if (rows < 1 || out_features < 1 || in_features < 16 || in_features % 16 || in_features > 131056 || rows > LONGEST || out_features > LONGEST ||
-        (long)rows * out_features > 1l << 37)
-        return KOALA_E_SHAPE;
-    const Plan p = plan_of(rows, out_features, in_features);
-    *out = p.splits > 1 ? (size_t)p.splits * rows * ((out_features + 3) / 4) * 16 : 0;
-    return KOALA_OK;
+    Plan p;
+    return planned(rows, out_features, in_features, &p, out);
 }
 
 koala_status koala_linear_quantized(void *hip_stream, int rows, int out_features, int in_features, const int8_t *q, int64_t q_stride,
@@ -791,7 +794,8 @@ koala_status koala_linear_quantized(void *hip_stream, int rows, int out_features
     if (!q || !q_scale || !w || !w_scale || !y) return KOALA_E_NULL;
     if (y_dtype != KOALA_FP32 && y_dtype != KOALA_BF16) return KOALA_E_UNSUPPORTED;
     size_t need = 0;
-    const koala_status rc = koala_linear_workspace_bytes(rows, out_features, in_features, &need);
+    Plan p;
+    const koala_status rc = planned(rows, out_features, in_features, &p, &need);
     if (rc != KOALA_OK) return rc;
     if (q_stride < in_features || w_stride < in_features || y_stride < out_features) return KOALA_E_SHAPE;
     const uintptr_t unit = y_dtype == KOALA_FP32 ? 4 : 2;
@@ -800,7 +804,6 @@ koala_status koala_linear_quantized(void *hip_stream, int rows, int out_features
         return KOALA_E_ALIGN;
     if (q_stride > (1 << 22) || w_stride > (1 << 22)) return KOALA_E_SHAPE;   // 256 rows' bytes are counted in 31 bits
     if (need > 0 && (!workspace || workspace_bytes < need)) return KOALA_E_WORKSPACE;
-    const Plan p = plan_of(rows, out_features, in_features);
     LinearArgs a{q, w, (size_t)q_stride, (size_t)w_stride, (size_t)y_stride, q_scale, w_scale, add, y, rows, out_features, in_features, y_dtype == KOALA_FP32,
                  p.splits, (int *)workspace};
     hipStream_t st = (hipStream_t)hip_stream;
